@@ -526,6 +526,89 @@ slimdp_status slimdp_round_host(float* w_host, const float* const* grads_host, u
                                 uint32_t* core_idx_host, uint32_t* const* exp_idx_host,
                                 float* const* pulled_host, void* arena, size_t arena_bytes, void* stream);
 
+/* ==================================================== a worker's local step ===
+ * The round moves updates that local training has made; the calls below make
+ * them.  They compute the residual feed-forward part of a network and its loss,
+ * forward and backward, on row-major matrices: `x [rows, cols], ldx` is a matrix
+ * whose row r starts ldx elements after row r - 1 (ldx >= cols); columns are
+ * adjacent.  A call's matrices hold `type` elements; everything a worker pushes
+ * or pulls as a vector (gamma, beta, bias and the gradients of all parameters)
+ * is fp32, so that it can live in slices of the flat model and of the flat
+ * update, at any 4-byte aligned offset.  Matrices need their element's alignment
+ * only; 16-byte aligned rows are faster.  Sums and statistics are fp32 or wider,
+ * and a result is rounded once, when it is stored.
+ *   accumulate != 0: a parameter gradient is added to what its buffer holds.
+ *   rows or m = 0 is legal: parameter gradients become (or stay, with
+ *   accumulate) what an empty sum leaves. */
+enum { SLIMDP_F32 = 0, SLIMDP_BF16 = 1, SLIMDP_F16 = 2 };                       /* type */
+enum { SLIMDP_ACT_NONE = 0, SLIMDP_ACT_RELU = 1, SLIMDP_ACT_GELU = 2,           /* z Phi(z) with erf */
+       SLIMDP_ACT_GELU_TANH = 3,                                                /* its tanh form     */
+       SLIMDP_ACT_SILU = 4 };                                                   /* z / (1 + exp(-z)) */
+
+/* Layer norm over the last dimension, 1 <= dim < 2^31, rows < 2^31:
+ *   mean = sum x / dim;  rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps);  h = (x - mean) rstd
+ *   y = h gamma + beta
+ * gamma, beta [dim] or NULL (1 and 0); mean, rstd [rows] (written) or NULL; eps finite, >= 0.
+ * backward, with the forward's mean and rstd and g = dy gamma:
+ *   dx = rstd (g - avg(g) - h avg(g h));  dgamma (+)= sum over rows of dy h;  dbeta (+)= sum over rows of dy
+ * dgamma and dbeta [dim] or NULL.  ws: slimdp_layernorm_workspace_bytes(rows, dim) bytes, 16-byte aligned
+ * (unused, may be NULL, where dgamma and dbeta are both NULL). */
+size_t slimdp_layernorm_workspace_bytes(uint64_t rows, uint64_t dim);
+slimdp_status slimdp_layernorm_forward(const void* x, uint64_t ldx, uint64_t rows, uint64_t dim, int32_t type,
+                                       const float* gamma, const float* beta, float eps, void* y, uint64_t ldy,
+                                       float* mean, float* rstd, void* stream);
+slimdp_status slimdp_layernorm_backward(const void* dy, uint64_t lddy, const void* x, uint64_t ldx, uint64_t rows,
+                                        uint64_t dim, int32_t type, const float* gamma, const float* mean,
+                                        const float* rstd, void* dx, uint64_t lddx, float* dgamma, float* dbeta,
+                                        int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Matrix product of a layer with n outputs and k inputs, w [n, k], 1 <= n, k < 2^31, m < 2^31:
+ *   forward           z = x w^T + bias;  y = act(z) + residual             x [m, k], y, z, residual [m, n]
+ *   backward_input    dx = (dy w) * act'(z) + add                          dy [m, n], dx, z, add [m, k]
+ *   backward_weight   dw (+)= dy^T x;  db (+)= sum over rows of dy         dw [n, k] fp32, db [n]
+ *   activation_backward  dz = dy * act'(z)                                 [m, n], for a product that ends a chain
+ * bias, residual, add, db and the forward's z (written: the pre-activation, for the gradient) may be NULL.
+ * backward_input's z is the pre-activation of the layer that made x, and act that layer's activation, so that dx
+ * is that layer's dz; z may be NULL only where act is SLIMDP_ACT_NONE.  relu'(0) = 0.
+ * 16-bit types are multiplied exactly and summed in fp32.  fp32 matrices are split into three bf16 parts
+ * each, which hold 24 bits between them; the six largest of the nine products of parts are summed, which
+ * leaves an error of the order of fp32's own rounding.  An infinity in an fp32 matrix makes the results it reaches NaN
+ * or infinite.  ws: slimdp_linear_workspace_bytes(m, n, k, type) bytes, 256-byte aligned. */
+size_t slimdp_linear_workspace_bytes(uint64_t m, uint64_t n, uint64_t k, int32_t type);
+slimdp_status slimdp_linear_forward(const void* x, uint64_t ldx, const void* w, uint64_t ldw, const float* bias,
+                                    const void* residual, uint64_t ldr, uint64_t m, uint64_t n, uint64_t k,
+                                    int32_t type, int32_t act, void* y, uint64_t ldy, void* z, uint64_t ldz, void* ws,
+                                    size_t ws_bytes, void* stream);
+slimdp_status slimdp_linear_backward_input(const void* dy, uint64_t lddy, const void* w, uint64_t ldw, const void* z,
+                                           uint64_t ldz, const void* add, uint64_t ldadd, uint64_t m, uint64_t n,
+                                           uint64_t k, int32_t type, int32_t act, void* dx, uint64_t lddx, void* ws,
+                                           size_t ws_bytes, void* stream);
+slimdp_status slimdp_linear_backward_weight(const void* dy, uint64_t lddy, const void* x, uint64_t ldx, uint64_t m,
+                                            uint64_t n, uint64_t k, int32_t type, float* dw, uint64_t lddw, float* db,
+                                            int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+slimdp_status slimdp_activation_backward(const void* dy, uint64_t lddy, const void* z, uint64_t ldz, uint64_t m,
+                                         uint64_t n, int32_t type, int32_t act, void* dz, uint64_t lddz, void* stream);
+
+/* Distillation from a teacher's top logits, with hard labels beside them, loss and gradient in one call.
+ * Row r has logits s [vocab], the teacher's entries (teacher_idx[r][j], teacher_logit[r][j]), j < top, a label
+ * and a weight; T = temperature, p^T = softmax(s / T), p = softmax(s), q = softmax over the entries that are there
+ * of teacher_logit / T:
+ *   loss[r] = weight ( kd T^2 sum_j q_j (log q_j - log p^T[idx_j]) - ce log p[label] )
+ *   dlogits[r][i] = weight ( kd T (p^T_i - sum over j with idx_j = i of q_j) + ce (p_i - [i = label]) )
+ * An index or a label outside [0, vocab) is absent.  A row without entries has no first term, a row without a
+ * label (or label = NULL) no second one; a row with neither term, with weight 0, or with nothing but -inf among its
+ * logits has loss and gradient 0.  q_j = 0 adds 0, whatever p^T is there.  Entries may repeat an index.
+ *   logits, dlogits [rows, vocab] of `type`, 1 <= vocab < 2^31, rows < 2^31; dlogits = NULL: the loss alone;
+ *   dlogits may be logits (same ld)
+ *   teacher_idx [rows, top] int32, teacher_logit [rows, top] of `teacher_type`, both without row padding,
+ *   0 <= top <= SLIMDP_MAX_TOP; label [rows] int32 or NULL; row_weight [rows] or NULL (1)
+ *   temperature finite, > 0; kd_weight, ce_weight finite; loss [rows] fp32 (written) */
+#define SLIMDP_MAX_TOP 1024
+slimdp_status slimdp_distill(const void* logits, uint64_t ldl, uint64_t rows, uint64_t vocab, int32_t type,
+                             const int32_t* teacher_idx, const void* teacher_logit, int32_t teacher_type, uint32_t top,
+                             const int32_t* label, const float* row_weight, float temperature, float kd_weight,
+                             float ce_weight, float* loss, void* dlogits, uint64_t ldd, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

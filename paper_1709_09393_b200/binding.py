@@ -24,6 +24,7 @@ lib = ctypes.CDLL(_LIB_PATH)
 _vp = ctypes.c_void_p
 _u64 = ctypes.c_uint64
 _u32 = ctypes.c_uint32
+_i32 = ctypes.c_int32
 _f32 = ctypes.c_float
 _sz = ctypes.c_size_t
 _pp = ctypes.POINTER(ctypes.c_void_p)
@@ -79,6 +80,20 @@ EXPORTS = {
     "slimdp_mark_dominant_kernel": (None, [_vp, _vp]),
     "slimdp_round_host": (ctypes.c_int32, [_vp, _pp, _u32, _u64, _f32, _u64, _u64, _u64, _u32, _f32, _vp, _pp, _pp,
                                            _vp, _sz, _vp]),
+    "slimdp_layernorm_workspace_bytes": (_sz, [_u64, _u64]),
+    "slimdp_layernorm_forward": (_i32, [_vp, _u64, _u64, _u64, _i32, _vp, _vp, _f32, _vp, _u64, _vp, _vp, _vp]),
+    "slimdp_layernorm_backward": (_i32, [_vp, _u64, _vp, _u64, _u64, _u64, _i32, _vp, _vp, _vp, _vp, _u64, _vp, _vp,
+                                         _i32, _vp, _sz, _vp]),
+    "slimdp_linear_workspace_bytes": (_sz, [_u64, _u64, _u64, _i32]),
+    "slimdp_linear_forward": (_i32, [_vp, _u64, _vp, _u64, _vp, _vp, _u64, _u64, _u64, _u64, _i32, _i32, _vp, _u64,
+                                     _vp, _u64, _vp, _sz, _vp]),
+    "slimdp_linear_backward_input": (_i32, [_vp, _u64, _vp, _u64, _vp, _u64, _vp, _u64, _u64, _u64, _u64, _i32, _i32,
+                                            _vp, _u64, _vp, _sz, _vp]),
+    "slimdp_linear_backward_weight": (_i32, [_vp, _u64, _vp, _u64, _u64, _u64, _u64, _i32, _vp, _u64, _vp, _i32, _vp,
+                                             _sz, _vp]),
+    "slimdp_activation_backward": (_i32, [_vp, _u64, _vp, _u64, _u64, _u64, _i32, _i32, _vp, _u64, _vp]),
+    "slimdp_distill": (_i32, [_vp, _u64, _u64, _u64, _i32, _vp, _vp, _i32, _u32, _vp, _vp, _f32, _f32, _f32, _vp, _vp,
+                              _u64, _vp]),
 }
 
 for _name, (_res, _args) in EXPORTS.items():

@@ -4,9 +4,13 @@
 //   backward_input   dx = (dy w) * act'(z) + add
 //   backward_weight  dw (+)= dy^T x, db (+)= sum over rows of dy
 //
-// All three are one product  C[i, j] = sum_l A(i, l) B(j, l)  over operands with two strides each.
+// All three are one product  C[i, j] = sum_l A(i, l) B(j, l); an operand's rows hold either the summed index (K-major)
+// or the kept one (MN-major), and TMA and the tensor cores read both.
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
+#include "tensor.cuh"
 #include "train.cuh"
 
 namespace slimdp {
@@ -25,61 +29,353 @@ struct Epilogue {
 
 enum Product { kForward, kInput, kWeight };
 
-template <typename T, Product P>
-__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint64_t j, float v) {
+// V adjacent results C[i, j .. j + V), through the epilogue of product P; bias: the V values of these columns.
+template <typename T, Product P, int V>
+__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint64_t j, float (&v)[V], const float (&bias)[V]) {
     if constexpr (P == kForward) {
-        if (e.bias) v += __ldg(e.bias + j);
-        if (e.z) ((T*)e.z)[i * e.ldz + j] = from_f32<T>(v);
-        v = act_value(v, e.act);
-        if (e.add) v += to_f32(((const T*)e.add)[i * e.ldadd + j]);
-        ((T*)e.out)[i * e.ldo + j] = from_f32<T>(v);
+#pragma unroll
+        for (int c = 0; c < V; ++c) v[c] += bias[c];
+        if (e.z) store_pack<T, V>((T*)e.z + i * e.ldz + j, v);
+        if (e.act != SLIMDP_ACT_NONE) {
+#pragma unroll
+            for (int c = 0; c < V; ++c) v[c] = act_value(v[c], e.act);
+        }
     } else if constexpr (P == kInput) {
-        if (e.act != SLIMDP_ACT_NONE) v *= act_slope(to_f32(((const T*)e.z)[i * e.ldz + j]), e.act);
-        if (e.add) v += to_f32(((const T*)e.add)[i * e.ldadd + j]);
-        ((T*)e.out)[i * e.ldo + j] = from_f32<T>(v);
-    } else {
+        if (e.act != SLIMDP_ACT_NONE) {
+            float z[V];
+            unpack<T, V>(load_pack<T, V>((const T*)e.z + i * e.ldz + j), z);
+#pragma unroll
+            for (int c = 0; c < V; ++c) v[c] *= act_slope(z[c], e.act);
+        }
+    }
+    if constexpr (P == kWeight) {
         float* o = (float*)e.out + i * e.ldo + j;
-        *o = e.accumulate ? *o + v : v;
+        if (e.accumulate) {
+            float old[V];
+            unpack<float, V>(load_pack<float, V>(o), old);
+#pragma unroll
+            for (int c = 0; c < V; ++c) v[c] += old[c];
+        }
+        store_pack<float, V>(o, v);
+    } else {
+        if (e.add) {
+            float a[V];
+            unpack<T, V>(load_pack<T, V>((const T*)e.add + i * e.ldadd + j), a);
+#pragma unroll
+            for (int c = 0; c < V; ++c) v[c] += a[c];
+        }
+        store_pack<T, V>((T*)e.out + i * e.ldo + j, v);
     }
 }
 
-template <typename T>
-struct Operand {
-    const T* p;
-    uint64_t row, col;   // strides of the kept and of the summed index
+// Elements of the type that product P stores that make 16 bytes.
+template <typename T, Product P>
+constexpr int kWide = P == kWeight ? 4 : kVec<T>;
+
+constexpr int kBk = 64;                      // summed indices of a stage: 128 bytes of a 16-bit type
+constexpr uint32_t kChunk = 8;               // blocks of kBk summed indices that stay in one accumulator where T or P asks for fp32 results
+constexpr int kEpilogueWarps = 8;
+constexpr int kProductThreads = 32 * (2 + kEpilogueWarps);
+constexpr int kEpiloguePitch = 33;           // floats of a row of a warp's 32 x 32 staging square
+
+// A wait in a product kernel ran out on this device (never, unless the device misbehaves).
+__device__ int g_product_status;
+
+struct ProductArgs {
+    uint64_t m, n;
+    uint32_t tiles_m, tiles_n, kblocks, splits;
+    uint32_t format;          // of the instruction descriptor: 1 = bf16, 0 = fp16
+    bool wide;                // rows of all tensors of the epilogue start on 16-byte boundaries
+    float* partial;           // [splits][m][ld_partial] sums that a second kernel joins, or NULL
+    uint64_t ld_partial;
+    Epilogue e;
 };
 
-// 64 x 64 results a CTA, 4 x 4 a thread, 16 summed indices a step.
-template <typename T, Product P>
-__global__ void __launch_bounds__(256) product_kernel(Operand<T> a, Operand<T> b, uint64_t m, uint64_t n, uint64_t k,
-                                                      Epilogue e) {
-    __shared__ float sa[16][65], sb[16][65];
-    const uint64_t i0 = (uint64_t)blockIdx.y * 64, j0 = (uint64_t)blockIdx.x * 64;
-    const uint32_t ti = threadIdx.x / 16, tj = threadIdx.x % 16;
-    float acc[4][4] = {};
-    for (uint64_t l0 = 0; l0 < k; l0 += 16) {
-        for (uint32_t s = threadIdx.x; s < 64 * 16; s += 256) {
-            const uint32_t r = a.col == 1 ? s / 16 : s % 64, c = a.col == 1 ? s % 16 : s / 64;
-            sa[c][r] = (i0 + r < m && l0 + c < k) ? to_f32(a.p[(i0 + r) * a.row + (l0 + c) * a.col]) : 0.0f;
-        }
-        for (uint32_t s = threadIdx.x; s < 64 * 16; s += 256) {
-            const uint32_t r = b.col == 1 ? s / 16 : s % 64, c = b.col == 1 ? s % 16 : s / 64;
-            sb[c][r] = (j0 + r < n && l0 + c < k) ? to_f32(b.p[(j0 + r) * b.row + (l0 + c) * b.col]) : 0.0f;
-        }
-        __syncthreads();
+// V results of one row, or as many as the row has left.
+template <typename T, Product P, int V>
+__device__ __forceinline__ void finish_columns(const ProductArgs& args, uint64_t i, uint64_t j, float (&v)[V]) {
+    const float* bias = P == kForward ? args.e.bias : nullptr;
+    if (j + V <= args.n) {
+        float b[V];
 #pragma unroll
-        for (int c = 0; c < 16; ++c)
+        for (int c = 0; c < V; ++c) b[c] = bias ? __ldg(bias + j + c) : 0.0f;
+        finish<T, P, V>(args.e, i, j, v, b);
+    } else {
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(sa[c][ti * 4 + u], sb[c][tj * 4 + v], acc[u][v]);
-        __syncthreads();
+        for (int c = 0; c < V; ++c)
+            if (j + c < args.n) {
+                float one[1] = {v[c]}, b[1] = {bias ? __ldg(bias + j + c) : 0.0f};
+                finish<T, P, 1>(args.e, i, j + c, one, b);
+            }
     }
-    for (int u = 0; u < 4; ++u)
-        for (int v = 0; v < 4; ++v) {
-            const uint64_t i = i0 + ti * 4 + u, j = j0 + tj * 4 + v;
-            if (i < m && j < n) finish<T, P>(e, i, j, acc[u][v]);
+}
+
+// A warp's 32 x 32 results, row-wise in shared memory: V adjacent columns a lane, so that a warp's accesses to memory
+// cover whole rows of the square.
+template <typename T, Product P, int V, bool PARTIAL>
+__device__ __forceinline__ void finish_square_by(const ProductArgs& args, uint32_t split, const float* square,
+                                                 uint64_t row0, uint64_t col0, uint32_t lane) {
+    const uint32_t c = lane % (32 / V) * V, r = lane / (32 / V);
+    if (col0 + c >= args.n) return;
+#pragma unroll 1
+    for (uint32_t r0 = r; r0 < 32; r0 += V) {
+        const uint64_t i = row0 + r0;
+        if (i >= args.m) break;
+        float v[V];
+#pragma unroll
+        for (int u = 0; u < V; ++u) v[u] = square[r0 * kEpiloguePitch + c + u];
+        if constexpr (PARTIAL)
+            store_pack<float, V>(args.partial + ((uint64_t)split * args.m + i) * args.ld_partial + col0 + c, v);
+        else
+            finish_columns<T, P, V>(args, i, col0 + c, v);
+    }
+}
+
+template <typename T, Product P>
+__device__ __forceinline__ void finish_square(const ProductArgs& args, uint32_t split, const float* square, uint64_t row0,
+                                              uint64_t col0, uint32_t lane) {
+    if (args.partial)
+        finish_square_by<T, P, 4, true>(args, split, square, row0, col0, lane);
+    else if (args.wide)
+        finish_square_by<T, P, kWide<T, P>, false>(args, split, square, row0, col0, lane);
+    else
+        finish_square_by<T, P, 1, false>(args, split, square, row0, col0, lane);
+}
+
+template <int CG, int BN>
+struct ProductShape {
+    static constexpr uint32_t a_bytes = 128 * kBk * 2, b_bytes = BN / CG * kBk * 2, stage = a_bytes + b_bytes;
+    static constexpr uint32_t epilogue = kEpilogueWarps * 32 * kEpiloguePitch * 4, control = 512;
+    static constexpr uint32_t stages = (232448 - 1024 - epilogue - control) / stage < 8 ? (232448 - 1024 - epilogue - control) / stage : 8;
+    static constexpr uint32_t smem = stages * stage + epilogue + control + 1024;
+    static constexpr uint32_t columns = 2 * BN;     // two accumulators
+};
+
+// The parts of the two operands that the six products of a block of summed indices take, smallest first.
+__device__ __forceinline__ uint32_t part_a(int p) { return (0x021010u >> (4 * (5 - p))) & 0xFu; }
+__device__ __forceinline__ uint32_t part_b(int p) { return (0x201100u >> (4 * (5 - p))) & 0xFu; }
+
+// The tensor cores cut, rather than round, every 16-index sum to the accumulator's 24 bits: measured, a relative error of
+// 1.7e-8 towards zero for each, 2.9e-5 after 4096 indices of six products.  Results of 16 bits do not show it.  For fp32
+// results the accumulator is emptied every kChunk blocks into sums in registers, which round to nearest.
+template <typename T, Product P>
+constexpr bool kChunked = P == kWeight || sizeof(T) == 4;
+
+// Tile number -> (row, column) of tiles: eight rows of tiles are walked column by column, so that the tiles that run
+// at one time share their operands in L2.
+__device__ __forceinline__ void tile_place(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+    const uint32_t band = t / (8 * tiles_n), first = band * 8, height = min(8u, tiles_m - first), in = t - band * 8 * tiles_n;
+    tm = first + in % height;
+    tn = in / height;
+}
+
+// One 128 CG x BN tile at a time: warp 0 loads, warp 1 of the (leading) CTA multiplies, warps 2 to 9 finish.
+template <typename T, Product P, int CG, int BN>
+__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ CUtensorMap map_a,
+                                                                     const __grid_constant__ CUtensorMap map_b,
+                                                                     const ProductArgs args) {
+    using S = ProductShape<CG, BN>;
+    constexpr bool kMnA = P == kWeight, kMnB = P != kForward;
+    constexpr int kParts = sizeof(T) == 4 ? 6 : 1;     // products of operand parts
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
+    uint8_t* const smem = raw + (base - smem_addr(raw));
+    const uint32_t control = base + S::stages * S::stage + S::epilogue;
+    auto full = [&](uint32_t s) { return control + 8 * s; };
+    auto empty = [&](uint32_t s) { return control + 64 + 8 * s; };
+    auto acc_full = [&](uint32_t b) { return control + 128 + 8 * b; };
+    auto acc_empty = [&](uint32_t b) { return control + 144 + 8 * b; };
+    const uint32_t slot = control + 160;
+
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    const uint32_t group = blockIdx.x / CG, groups = gridDim.x / CG;
+    const uint32_t items = args.tiles_m * args.tiles_n * args.splits;
+
+    if (warp == 0 && lane == 0) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+        for (uint32_t s = 0; s < S::stages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
         }
+        for (uint32_t b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_empty(b), CG * kEpilogueWarps);
+        }
+        mbar_init_fence();
+    }
+    if (warp == 1) tmem_alloc<CG>(slot, S::columns);
+    tc_fence_before();
+    __syncthreads();
+    __syncwarp();
+    if constexpr (CG == 2) cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem + (slot - base));
+
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t s = 0, phase = 0;
+            for (uint32_t item = group; item < items && ok; item += groups) {
+                uint32_t tm, tn;
+                tile_place(item / args.splits, args.tiles_m, args.tiles_n, tm, tn);
+                const uint32_t split = item % args.splits;
+                const uint32_t k0 = (uint32_t)((uint64_t)args.kblocks * split / args.splits);
+                const uint32_t k1 = (uint32_t)((uint64_t)args.kblocks * (split + 1) / args.splits);
+                const int32_t row_a = (int32_t)((tm * CG + rank) * 128), row_b = (int32_t)(tn * BN + rank * (BN / CG));
+                // fp32: the five small products of a chunk come first, so that only the large one meets a full accumulator
+                const uint32_t chunk = kChunked<T, P> ? kChunk : args.kblocks;
+                for (uint32_t c0 = k0; c0 < k1 && ok; c0 += chunk)
+                    for (int p = 0; p < kParts && ok; ++p)
+                        for (uint32_t kb = c0; kb < min(c0 + chunk, k1); ++kb) {
+                            if (!(ok = mbar_wait(empty(s), phase ^ 1u))) break;
+                            const uint32_t bar = CG == 2 ? cluster_addr(full(s), 0) : full(s);
+                            if (rank == 0) mbar_expect_tx(full(s), CG * S::stage);
+                            const uint32_t a = base + s * S::stage, b = a + S::a_bytes;
+                            const int32_t k = (int32_t)(kb * kBk);
+                            const int32_t pa = kParts > 1 ? (int32_t)part_a(p) : 0, pb = kParts > 1 ? (int32_t)part_b(p) : 0;
+                            if constexpr (kMnA) {
+#pragma unroll
+                                for (int c = 0; c < 2; ++c) tma_load<CG == 2>(a + c * 64 * kBk * 2, &map_a, row_a + c * 64, k, pa, bar);
+                            } else {
+                                tma_load<CG == 2>(a, &map_a, k, row_a, pa, bar);
+                            }
+                            if constexpr (kMnB) {
+#pragma unroll
+                                for (int c = 0; c < BN / CG / 64; ++c) tma_load<CG == 2>(b + c * 64 * kBk * 2, &map_b, row_b + c * 64, k, pb, bar);
+                            } else {
+                                tma_load<CG == 2>(b, &map_b, k, row_b, pb, bar);
+                            }
+                            if (++s == S::stages) s = 0, phase ^= 1u;
+                        }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = (1u << 4) | (args.format << 7) | (args.format << 10) | ((kMnA ? 1u : 0u) << 15) |
+                                   ((kMnB ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 * CG >> 4) << 24);
+            constexpr uint32_t step_a = (kMnA ? 2048u : 32u) >> 4, step_b = (kMnB ? 2048u : 32u) >> 4;
+            uint32_t s = 0, phase = 0, count = 0;
+            for (uint32_t item = group; item < items && ok; item += groups) {
+                const uint32_t split = item % args.splits;
+                const uint32_t k0 = (uint32_t)((uint64_t)args.kblocks * split / args.splits);
+                const uint32_t k1 = (uint32_t)((uint64_t)args.kblocks * (split + 1) / args.splits);
+                const uint32_t chunk = kChunked<T, P> ? kChunk : args.kblocks;
+                for (uint32_t c0 = k0; c0 < k1 && ok; c0 += chunk, ++count) {
+                    const uint32_t steps = (min(c0 + chunk, k1) - c0) * kParts, buf = count & 1u;
+                    if (!(ok = mbar_wait(acc_empty(buf), ((count >> 1) & 1u) ^ 1u))) break;
+                    tc_fence_after();
+                    for (uint32_t i = 0; i < steps; ++i) {
+                        if (!(ok = mbar_wait(full(s), phase))) break;
+                        tc_fence_after();
+                        const uint32_t a = base + s * S::stage, b = a + S::a_bytes;
+                        const uint64_t da = operand_desc(a, kMnA, 64 * kBk * 2), db = operand_desc(b, kMnB, 64 * kBk * 2);
+#pragma unroll
+                        for (int u = 0; u < kBk / 16; ++u)
+                            tc_mma<CG>(tmem + buf * BN, da + u * step_a, db + u * step_b, idesc, i > 0 || u > 0);
+                        tc_commit<CG>(empty(s));
+                        if (++s == S::stages) s = 0, phase ^= 1u;
+                    }
+                    if (ok) tc_commit<CG>(acc_full(buf));
+                }
+            }
+        }
+    } else {
+        const uint32_t quarter = warp & 3u, half = (warp - 2) >> 2;
+        float* const square = reinterpret_cast<float*>(smem + S::stages * S::stage) + (warp - 2) * 32 * kEpiloguePitch;
+        constexpr int kSquares = BN / 64;             // of 32 x 32 results of this warp
+        const uint32_t lanes = tmem + ((quarter * 32) << 16) + half * (BN / 2);
+        uint32_t count = 0;
+        for (uint32_t item = group; item < items && ok; item += groups) {
+            uint32_t tm, tn;
+            tile_place(item / args.splits, args.tiles_m, args.tiles_n, tm, tn);
+            const uint32_t split = item % args.splits;
+            const uint64_t row0 = (uint64_t)(tm * CG + rank) * 128 + quarter * 32, col0 = (uint64_t)tn * BN + half * (BN / 2);
+            if constexpr (kChunked<T, P>) {
+                const uint32_t k0 = (uint32_t)((uint64_t)args.kblocks * split / args.splits);
+                const uint32_t k1 = (uint32_t)((uint64_t)args.kblocks * (split + 1) / args.splits);
+                float sum[kSquares][32];
+#pragma unroll
+                for (int q = 0; q < kSquares; ++q)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) sum[q][c] = 0.0f;
+                for (uint32_t c0 = k0; c0 < k1; c0 += kChunk, ++count) {
+                    if (!(ok = mbar_wait(acc_full(count & 1u), (count >> 1) & 1u))) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int q = 0; q < kSquares; ++q) {
+                        float v[32];
+                        tmem_load32(lanes + (count & 1u) * BN + q * 32, v);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) sum[q][c] += v[c];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(cluster_addr(acc_empty(count & 1u), 0));
+                }
+                if (!ok) break;
+#pragma unroll 1
+                for (int q = 0; q < kSquares; ++q) {
+#pragma unroll
+                    for (int u = 0; u < kSquares; ++u)
+                        if (u == q) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) square[lane * kEpiloguePitch + c] = sum[u][c];
+                        }
+                    __syncwarp();
+                    finish_square<T, P>(args, split, square, row0, col0 + q * 32, lane);
+                    __syncwarp();
+                }
+            } else {
+                const uint32_t buf = count & 1u;
+                if (!(ok = mbar_wait(acc_full(buf), (count >> 1) & 1u))) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int q = 0; q < kSquares; ++q) {
+                    {
+                        float v[32];
+                        tmem_load32(lanes + buf * BN + q * 32, v);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) square[lane * kEpiloguePitch + c] = v[c];
+                    }
+                    if (q == kSquares - 1) tc_fence_before();      // the accumulator has been read
+                    __syncwarp();
+                    if (q == kSquares - 1 && lane == 0) mbar_arrive_cluster(cluster_addr(acc_empty(buf), 0));
+                    finish_square<T, P>(args, split, square, row0, col0 + q * 32, lane);
+                    __syncwarp();
+                }
+                ++count;
+            }
+        }
+    }
+
+    if (!ok) {
+        atomicExch(&g_product_status, SLIMDP_ERR_INTERNAL);
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);     // copies and products under way end meanwhile
+    }
+    tc_fence_before();
+    __syncthreads();
+    __syncwarp();
+    if constexpr (CG == 2) cluster_sync();
+    if (warp == 1) tmem_free<CG>(tmem, S::columns);
+    if constexpr (CG == 2) cluster_sync();      // neither CTA of a pair leaves before both have freed
+}
+
+// Joins the sums of `splits` parts of the summed axis and finishes them.
+template <typename T, Product P, int V>
+__global__ void __launch_bounds__(256) join_kernel(const ProductArgs args) {
+    const uint64_t pieces = (args.n + V - 1) / V, total = pieces * args.m;
+    for (uint64_t p = (uint64_t)blockIdx.x * 256 + threadIdx.x; p < total; p += (uint64_t)gridDim.x * 256) {
+        const uint64_t i = p / pieces, j = (p - i * pieces) * V;
+        float v[V] = {};
+        for (uint32_t s = 0; s < args.splits; ++s) {
+            const float* src = args.partial + ((uint64_t)s * args.m + i) * args.ld_partial + j;
+#pragma unroll
+            for (int c = 0; c < V; ++c) v[c] += src[c];       // ld_partial is a multiple of V: in bounds
+        }
+        finish_columns<T, P, V>(args, i, j, v);
+    }
 }
 
 // db (+)= sum over rows of dy: a CTA takes 32 columns, its 32 warps every 32nd row each.
@@ -111,19 +407,221 @@ __global__ void __launch_bounds__(256) activation_backward_kernel(const T* __res
         }
 }
 
+// ---- operands
+
+struct Matrix {
+    const void* p;
+    uint64_t ld, rows, cols;
+};
+
+// Operands that TMA cannot read in place: rows that do not start on 16-byte boundaries are copied to rows that do.
+template <typename T>
+__global__ void __launch_bounds__(256) align_kernel(const T* __restrict__ src, uint64_t ld, uint64_t rows, uint64_t cols,
+                                                    T* __restrict__ dst, uint64_t ld_dst) {
+    for (uint64_t i = blockIdx.y; i < rows; i += gridDim.y)
+        for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < cols; j += (uint64_t)gridDim.x * 256)
+            dst[i * ld_dst + j] = src[i * ld + j];
+}
+
+// fp32 = three bf16 parts, each the leading eight bits of what the ones before leave: cut, not rounded, so that no part
+// of a finite number overflows; the parts of a number without a finite leading part are that part and zeros.
+__global__ void __launch_bounds__(256) parts_kernel(const float* __restrict__ src, uint64_t ld, uint64_t rows, uint64_t cols,
+                                                    __nv_bfloat16* __restrict__ dst, uint64_t ld_dst) {
+    for (uint64_t i = blockIdx.y; i < rows; i += gridDim.y)
+        for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < cols; j += (uint64_t)gridDim.x * 256) {
+            float v = src[i * ld + j];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const float head = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+                const bool finite = fabsf(v) <= 3.4028234663852886e38f;
+                __nv_bfloat16 h = finite ? (p < 2 ? __float2bfloat16_rz(head) : __float2bfloat16_rn(v)) : __float2bfloat16_rn(v);
+                dst[((uint64_t)p * rows + i) * ld_dst + j] = h;
+                v = finite ? v - __bfloat162float(h) : 0.0f;
+            }
+        }
+}
+
+uint64_t packed_ld(uint64_t cols) { return align_up(cols, 8); }
+size_t packed_bytes(uint64_t rows, uint64_t cols, int32_t type) {
+    return align_up(rows * packed_ld(cols) * 2 * (type == SLIMDP_F32 ? 3 : 1), 256);
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static std::atomic<void*> cached{nullptr};
+    void* f = cached.load(std::memory_order_relaxed);
+    if (!f) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        cached.store(f, std::memory_order_relaxed);
+    }
+    return (EncodeTiled)f;
+}
+
+// A matrix as TMA reads it, boxes of box_rows x 64 elements, `parts` planes of it one after the other.
+bool encode(CUtensorMap* map, const Matrix& a, bool f16, int parts, uint32_t box_rows) {
+    const EncodeTiled f = encode_tiled();
+    if (!f) return false;
+    const cuuint64_t dims[3] = {a.cols, a.rows, (cuuint64_t)parts}, strides[2] = {a.ld * 2, a.ld * a.rows * 2};
+    const cuuint32_t box[3] = {kBk, box_rows, 1}, ones[3] = {1, 1, 1};
+    return f(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.p), dims,
+             strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Takes scratch from the front of a workspace.
+struct Scratch {
+    uint8_t* p;
+    void* take(size_t bytes) {
+        void* r = p;
+        p += align_up(bytes, 256);
+        return r;
+    }
+};
+
+// Brings an operand into a form that TMA reads: in place where its rows start on 16-byte boundaries.
+template <typename T>
+slimdp_status prepare_operand(Matrix& a, Scratch& ws, cudaStream_t st) {
+    constexpr bool kSplit = sizeof(T) == 4;
+    if (!kSplit && aligned16(a.p) && a.ld % 8 == 0) return SLIMDP_OK;
+    const uint64_t ld = packed_ld(a.cols);
+    void* dst = ws.take(packed_bytes(a.rows, a.cols, kSplit ? SLIMDP_F32 : SLIMDP_BF16));
+    const dim3 grid((unsigned)std::min<uint64_t>((a.cols + 255) / 256, 64), (unsigned)std::min<uint64_t>(a.rows, 16384));
+    if constexpr (kSplit)
+        parts_kernel<<<grid, 256, 0, st>>>((const float*)a.p, a.ld, a.rows, a.cols, (__nv_bfloat16*)dst, ld);
+    else
+        align_kernel<T><<<grid, 256, 0, st>>>((const T*)a.p, a.ld, a.rows, a.cols, (T*)dst, ld);
+    SLIMDP_LAUNCHED(1);
+    a.p = dst;
+    a.ld = ld;
+    return SLIMDP_OK;
+}
+
+template <typename T, Product P, int CG, int BN>
+slimdp_status launch_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, const ProductArgs& args, uint32_t groups,
+                           cudaStream_t st) {
+    using S = ProductShape<CG, BN>;
+    static DeviceOnce once;
+    auto kernel = product_kernel<T, P, CG, BN>;
+    if (once.needed()) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem) != cudaSuccess) return SLIMDP_ERR_CUDA;
+        once.mark();
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(groups * CG);
+    cfg.blockDim = dim3(kProductThreads);
+    cfg.dynamicSmemBytes = S::smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, args) != cudaSuccess) return SLIMDP_ERR_CUDA;
+    SLIMDP_LAUNCHED(1);
+    return SLIMDP_OK;
+}
+
+constexpr uint64_t kPartialBytes = 64ull << 20;    // most scratch that a split of the summed axis takes
+
+// How the work is cut: tiles of 128 pair x width results, and `splits` parts of the summed axis.
+struct Plan {
+    uint32_t pair, width, splits;
+};
+
+uint64_t partial_bytes(uint64_t m, uint64_t n) { return m * align_up(n, 8) * 4; }
+
+Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks) {
+    const uint64_t sms = 148;
+    Plan p = {2, 256, 1};
+    const uint64_t big = ((m + 255) / 256) * ((n + 255) / 256);
+    if (big * 2 <= sms / 2 || m <= 128) p = {1, n > 64 && ((m + 127) / 128) * ((n + 127) / 128) >= sms ? 128u : 64u, 1};
+    const uint64_t tiles = ((m + 128 * p.pair - 1) / (128 * p.pair)) * ((n + p.width - 1) / p.width);
+    const uint64_t slots = sms / p.pair;
+    if (tiles * 2 <= slots) {
+        uint64_t s = std::min(slots / tiles, std::max<uint64_t>(kblocks / 4, 1));
+        s = std::min(s, kPartialBytes / partial_bytes(m, n));
+        if (s > 1) p.splits = (uint32_t)s;
+    }
+    return p;
+}
+
+// C [m, n] = sum over k; a and b hold k along their rows or, where they are MN-major, along their columns.
 template <typename T, Product P>
-slimdp_status launch_product(Operand<T> a, Operand<T> b, uint64_t m, uint64_t n, uint64_t k, const Epilogue& e,
+slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_t k, const Epilogue& e, Scratch ws,
                              cudaStream_t st) {
-    const dim3 grid((unsigned)((n + 63) / 64), (unsigned)((m + 63) / 64));
-    if (grid.y > 65535) return SLIMDP_ERR_UNSUPPORTED;
-    product_kernel<T, P><<<grid, 256, 0, st>>>(a, b, m, n, k, e);
+    constexpr bool kMnA = P == kWeight, kMnB = P != kForward, kF16 = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value;
+    constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+    slimdp_status s = prepare_operand<T>(a, ws, st);
+    if (s == SLIMDP_OK) s = prepare_operand<T>(b, ws, st);
+    if (s != SLIMDP_OK) return s;
+    ProductArgs args = {};
+    args.m = m;
+    args.n = n;
+    args.kblocks = (uint32_t)((k + kBk - 1) / kBk);
+    args.format = kF16 ? 0u : 1u;
+    args.e = e;
+    const uint64_t size = P == kWeight ? 4 : sizeof(T);
+    auto starts_wide = [&](const void* p, uint64_t ld) { return !p || (aligned16(p) && (ld * size) % 16 == 0); };
+    args.wide = starts_wide(e.out, e.ldo) && starts_wide(e.z, e.ldz) && starts_wide(e.add, e.ldadd);
+    const Plan plan = plan_product(m, n, args.kblocks);
+    args.splits = plan.splits;
+    args.tiles_m = (uint32_t)((m + 128 * plan.pair - 1) / (128 * plan.pair));
+    args.tiles_n = (uint32_t)((n + plan.width - 1) / plan.width);
+    if (args.splits > 1) {
+        args.ld_partial = align_up(n, 8);
+        args.partial = (float*)ws.take(args.splits * m * args.ld_partial * 4);
+    }
+    CUtensorMap map_a, map_b;
+    if (!encode(&map_a, a, kF16, kParts, kMnA ? kBk : 128) || !encode(&map_b, b, kF16, kParts, kMnB ? kBk : plan.width / plan.pair))
+        return SLIMDP_ERR_CUDA;
+    const uint32_t items = args.tiles_m * args.tiles_n * args.splits;
+    const int sms = sm_count();
+    if (sms <= 0) return SLIMDP_ERR_CUDA;
+    const uint32_t groups = std::min<uint32_t>(items, (uint32_t)sms / plan.pair);
+    if (plan.pair == 2)
+        s = launch_tiles<T, P, 2, 256>(map_a, map_b, args, groups, st);
+    else if (plan.width == 128)
+        s = launch_tiles<T, P, 1, 128>(map_a, map_b, args, groups, st);
+    else
+        s = launch_tiles<T, P, 1, 64>(map_a, map_b, args, groups, st);
+    if (s != SLIMDP_OK || args.splits == 1) return s;
+    constexpr int V = kWide<T, P>;
+    const uint64_t pieces = (args.wide ? (n + V - 1) / V : n) * m;
+    const unsigned ctas = (unsigned)std::min<uint64_t>((pieces + 255) / 256, (uint64_t)sms * 8);
+    if (args.wide)
+        join_kernel<T, P, V><<<ctas, 256, 0, st>>>(args);
+    else
+        join_kernel<T, P, 1><<<ctas, 256, 0, st>>>(args);
     SLIMDP_LAUNCHED(1);
     return SLIMDP_OK;
 }
 
 }  // namespace
 
-size_t linear_ws_bytes(uint64_t, uint64_t, uint64_t, int32_t) { return 256; }
+size_t linear_ws_bytes(uint64_t m, uint64_t n, uint64_t k, int32_t type) {
+    // two packed operands and the partial sums of a split, of whichever of the three products takes most
+    const uint64_t x = packed_bytes(m, k, type), w = packed_bytes(n, k, type), dy = packed_bytes(m, n, type);
+    auto partial = [](uint64_t rows, uint64_t cols, uint64_t summed) -> uint64_t {
+        if (rows == 0 || summed == 0) return 0;
+        const Plan p = plan_product(rows, cols, (summed + kBk - 1) / kBk);
+        return p.splits > 1 ? align_up(p.splits * partial_bytes(rows, cols), 256) : 0;
+    };
+    return 256 + std::max({x + w + partial(m, n, k), dy + w + partial(m, k, n), dy + x + partial(n, k, m)});
+}
+
+slimdp_status read_product_status(cudaStream_t st) {
+    int status = 0;
+    if (cudaStreamSynchronize(st) != cudaSuccess || cudaMemcpyFromSymbol(&status, g_product_status, sizeof(status)) != cudaSuccess)
+        return SLIMDP_ERR_CUDA;
+    return status;
+}
 
 slimdp_status launch_linear_forward(const void* x, uint64_t ldx, const void* w, uint64_t ldw, const float* bias,
                                     const void* residual, uint64_t ldr, uint64_t m, uint64_t n, uint64_t k,
@@ -133,7 +631,7 @@ slimdp_status launch_linear_forward(const void* x, uint64_t ldx, const void* w, 
     const Epilogue e = {bias, z, ldz, residual, ldr, y, ldy, act, false};
     return with_type(type, [&](auto v) {
         using T = decltype(v);
-        return launch_product<T, kForward>({(const T*)x, ldx, 1}, {(const T*)w, ldw, 1}, m, n, k, e, st);
+        return launch_product<T, kForward>({x, ldx, m, k}, {w, ldw, n, k}, m, n, k, e, Scratch{(uint8_t*)ws}, st);
     });
 }
 
@@ -145,7 +643,7 @@ slimdp_status launch_linear_backward_input(const void* dy, uint64_t lddy, const 
     const Epilogue e = {nullptr, const_cast<void*>(z), ldz, add, ldadd, dx, lddx, act, false};
     return with_type(type, [&](auto v) {
         using T = decltype(v);
-        return launch_product<T, kInput>({(const T*)dy, lddy, 1}, {(const T*)w, 1, ldw}, m, k, n, e, st);
+        return launch_product<T, kInput>({dy, lddy, m, n}, {w, ldw, n, k}, m, k, n, e, Scratch{(uint8_t*)ws}, st);
     });
 }
 
@@ -160,7 +658,9 @@ slimdp_status launch_linear_backward_weight(const void* dy, uint64_t lddy, const
             column_sum_kernel<T><<<(unsigned)((n + 31) / 32), 1024, 0, st>>>((const T*)dy, lddy, m, n, db, accumulate);
             SLIMDP_LAUNCHED(1);
         }
-        return launch_product<T, kWeight>({(const T*)dy, 1, lddy}, {(const T*)x, 1, ldx}, n, k, m, e, st);
+        if (m == 0)
+            return cudaMemset2DAsync(dw, lddw * 4, 0, k * 4, n, st) == cudaSuccess ? SLIMDP_OK : SLIMDP_ERR_CUDA;
+        return launch_product<T, kWeight>({dy, lddy, m, n}, {x, ldx, m, k}, n, k, m, e, Scratch{(uint8_t*)ws}, st);
     });
 }
 

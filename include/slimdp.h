@@ -589,10 +589,6 @@ slimdp_status slimdp_linear_backward_weight(const void* dy, uint64_t lddy, const
 slimdp_status slimdp_activation_backward(const void* dy, uint64_t lddy, const void* z, uint64_t ldz, uint64_t m,
                                          uint64_t n, int32_t type, int32_t act, void* dz, uint64_t lddz, void* stream);
 
-/* The product kernels' waits are bounded (two seconds).  Synchronises `stream`, then returns SLIMDP_ERR_INTERNAL if one
- * ever ran out on this device, SLIMDP_OK otherwise. */
-slimdp_status slimdp_linear_read_status(void* stream);
-
 /* Distillation from a teacher's top logits, with hard labels beside them, loss and gradient in one call.
  * Row r has logits s [vocab], the teacher's entries (teacher_idx[r][j], teacher_logit[r][j]), j < top, a label
  * and a weight; T = temperature, p^T = softmax(s / T), p = softmax(s), q = softmax over the entries that are there
@@ -612,6 +608,10 @@ slimdp_status slimdp_distill(const void* logits, uint64_t ldl, uint64_t rows, ui
                              const int32_t* teacher_idx, const void* teacher_logit, int32_t teacher_type, uint32_t top,
                              const int32_t* label, const float* row_weight, float temperature, float kd_weight,
                              float ce_weight, float* loss, void* dlogits, uint64_t ldd, void* stream);
+
+/* The waits of the product and distillation kernels are bounded (two seconds).  Synchronises `stream`, then returns SLIMDP_ERR_INTERNAL if one
+ * ever ran out on this device, SLIMDP_OK otherwise. */
+slimdp_status slimdp_train_read_status(void* stream);
 
 #ifdef __cplusplus
 }

@@ -10,7 +10,7 @@ from .binding import (explore_shard_workspace_bytes, slimdp_sample_explore_shard
 from .driver import SlimDPDriver
 from .sharded import CudaBackend, select_core_sharded, shard_bounds, tie_quotas
 from .round import RoundBuffers, run_round
-from .train import (ACTIVATIONS, layernorm_workspace_bytes, linear_read_status, linear_workspace_bytes, slimdp_activation_backward,
+from .train import (ACTIVATIONS, layernorm_workspace_bytes, train_read_status, linear_workspace_bytes, slimdp_activation_backward,
                     slimdp_distill, slimdp_layernorm_backward, slimdp_layernorm_forward, slimdp_linear_backward_input,
                     slimdp_linear_backward_weight, slimdp_linear_forward)
 
@@ -22,7 +22,7 @@ __all__ = [
     "slimdp_select_core", "slimdp_sample_explore", "slimdp_sample_explore_batched", "slimdp_sample_explore_static", "slimdp_pack",
     "slimdp_core_signature", "wire_bytes", "slimdp_pack_batched", "slimdp_exchange", "slimdp_dense_merge_score", "slimdp_worker_merge_batched", "slimdp_merge", "slimdp_pull", "slimdp_pull_batched", "slimdp_round", "slimdp_round_host",
     "RoundBuffers", "run_round", "SlimDPDriver",
-    "ACTIVATIONS", "layernorm_workspace_bytes", "linear_read_status", "linear_workspace_bytes", "slimdp_activation_backward", "slimdp_distill",
+    "ACTIVATIONS", "layernorm_workspace_bytes", "train_read_status", "linear_workspace_bytes", "slimdp_activation_backward", "slimdp_distill",
     "slimdp_layernorm_backward", "slimdp_layernorm_forward", "slimdp_linear_backward_input",
     "slimdp_linear_backward_weight", "slimdp_linear_forward",
 ]

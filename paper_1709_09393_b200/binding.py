@@ -91,7 +91,7 @@ EXPORTS = {
                                             _vp, _u64, _vp, _sz, _vp]),
     "slimdp_linear_backward_weight": (_i32, [_vp, _u64, _vp, _u64, _u64, _u64, _u64, _i32, _vp, _u64, _vp, _i32, _vp,
                                              _sz, _vp]),
-    "slimdp_linear_read_status": (_i32, [_vp]),
+    "slimdp_train_read_status": (_i32, [_vp]),
     "slimdp_activation_backward": (_i32, [_vp, _u64, _vp, _u64, _u64, _u64, _i32, _i32, _vp, _u64, _vp]),
     "slimdp_distill": (_i32, [_vp, _u64, _u64, _u64, _i32, _vp, _vp, _i32, _u32, _vp, _vp, _f32, _f32, _f32, _vp, _vp,
                               _u64, _vp]),

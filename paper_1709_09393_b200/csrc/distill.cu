@@ -3,18 +3,25 @@
 // With T the temperature, p^T = softmax(s / T), p = softmax(s) and q the softmax of the teacher's entries / T:
 //   loss = w ( kd T^2 sum_j q_j (log q_j - log p^T[i_j]) - ce log p[y] )
 //   ds_i = w ( kd T (Q p^T_i - sum over j with i_j = i of q_j) + ce (p_i - [i = y]) ),  Q = sum_j q_j = 1 or 0.
-// Everywhere but at the teacher's entries and at the label the gradient is a multiple of the two softmaxes, so one
-// walk over the row yields the maximum and the two sums (kept relative to a running maximum, rescaled
-// where that rises) and a second walk writes the gradient; the few entries that have a term of their own are computed
-// from logits set aside before the second walk and stored after it, so that each result is rounded once.
+// Everywhere but at the teacher's entries and at the label the gradient is a multiple of the two softmaxes.  So a row
+// is read once and its exponentials stay in registers until its sums are known: a cluster of up to eight CTAs shares a
+// row, each holds a slice of at most 64 values a thread, and one exchange through distributed shared memory joins
+// maxima, sums and the loss's terms.  The few entries that have a term of their own are computed apart and stored over the
+// dense result, so that each value is rounded once.  A CTA walks over rows; the copy engine brings the slice of the
+// next row while this one is worked on.  Rows longer than a cluster holds are walked twice by one CTA.
 #include <algorithm>
+#include <atomic>
 #include <math.h>
 
+#include "tensor.cuh"
 #include "train.cuh"
 
 namespace slimdp {
 
 namespace {
+
+// A wait for a copy ran out on this device (never, unless the device misbehaves).
+__device__ int g_distill_status;
 
 constexpr int kDistillThreads = 512;
 constexpr int kDistillWarps = kDistillThreads / 32;
@@ -249,7 +256,591 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const T* logit
     if (tid == 0 && !label_done) out[y] = from_f32<T>(label_fix);
 }
 
+// Two fp32 values in one register pair; the packed instructions do both at the price of one.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split_pair(uint64_t p, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// A 16-byte piece of a row as four words; what the kernel needs to do with them, by type.
+template <typename T>
+struct Words;
+template <>
+struct Words<__nv_bfloat16> {
+    static constexpr uint32_t lowest = 0xFF80FF80u;     // -inf
+    static __device__ __forceinline__ uint32_t max(uint32_t a, uint32_t b) {
+        const __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+    static __device__ __forceinline__ float top(uint32_t a) { return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u)); }
+    // pair p of the piece
+    static __device__ __forceinline__ uint64_t pair(const uint32_t (&w)[4], int p) {
+        return pair_of(__uint_as_float(w[p] << 16), __uint_as_float(w[p] & 0xFFFF0000u));
+    }
+};
+template <>
+struct Words<__half> {
+    static constexpr uint32_t lowest = 0xFC00FC00u;
+    static __device__ __forceinline__ uint32_t max(uint32_t a, uint32_t b) {
+        const __half2 r = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+    static __device__ __forceinline__ float top(uint32_t a) {
+        const float2 f = __half22float2(*reinterpret_cast<__half2*>(&a));
+        return fmaxf(f.x, f.y);
+    }
+    static __device__ __forceinline__ uint64_t pair(const uint32_t (&w)[4], int p) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[p]));
+        return pair_of(f.x, f.y);
+    }
+};
+template <>
+struct Words<float> {
+    static constexpr uint32_t lowest = 0xFF800000u;
+    static __device__ __forceinline__ uint32_t max(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+    static __device__ __forceinline__ float top(uint32_t a) { return __uint_as_float(a); }
+    static __device__ __forceinline__ uint64_t pair(const uint32_t (&w)[4], int p) {
+        return pair_of(__uint_as_float(w[2 * p]), __uint_as_float(w[2 * p + 1]));
+    }
+};
+
+// Exponentials of a part of a row are kept as 2^(s c - K), K = m c rounded up to an integer, m the part's maximum: one
+// fused multiply-add each, and parts with different K differ by an exact power of two.  For an m that m c would not
+// hold (rows whose every logit is a mask's lowest value) they are 2^((s - m) c) instead.
+constexpr float kFar = 1.0e30f;
+
+__device__ __forceinline__ float reference(float m, float c) { return fabsf(m) < kFar ? ceilf(m * c) : 0.0f; }
+
+// What sums of a part with maximum m_part are multiplied by where they join a row with maximum m.
+__device__ __forceinline__ float rescale(float m_part, float m, float c) {
+    if (m_part == -INFINITY) return 1.0f;                       // the part's sums are 0, or NaN
+    if (!(fabsf(m) < kFar)) return exp2_approx((m_part - m) * c);
+    if (!(fabsf(m_part) < kFar)) return 0.0f;
+    return exp2_approx(ceilf(m_part * c) - ceilf(m * c));
+}
+
+// log of a row's sum of the power-th powers of 2^((s - m) c), from the sum as it is kept.
+__device__ __forceinline__ float log_sum(float sum, float m, float c, int power = 1) {
+    return logf(sum) - (fabsf(m) < kFar ? power * 0.69314718055994531f * fmaf(m, c, -ceilf(m * c)) : 0.0f);
+}
+
+// What is said in a cluster about a row.  A dense warp: its share's maximum and its sums relative to it, to every rank.
+// A teacher's warp: over the entries in its slice and relative to `kBase`, sum q and sum q (t - (s - base)), and the label's
+// logit, to rank 0; and to its own CTA what the row's gradient is multiplied by.
+enum { kMax, kSumT, kSum1, kVoice = 4 };
+enum { kBase, kQ, kTerm, kHasLabel, kLabel, kFacts = 8 };
+enum { kCoefT, kCoef1, kOwn = 4 };
+enum { kNoteTotal, kNoteLabel, kNote = 4 };     // from the first warp of the teacher's to the second
+
+// Slots of the table that finds entries with the same index: a power of two, at most half of them taken.
+__host__ __device__ inline uint32_t table_slots(uint32_t top) {
+    uint32_t n = 32;
+    while (n < 2 * top) n *= 2;
+    return n;
+}
+
+template <typename T, int WARPS, int PIECES>
+struct SliceShape {
+    static constexpr int elems = PIECES * kVec<T>;                       // of a thread
+    static constexpr uint32_t pieces = 32 * WARPS * PIECES, bytes = pieces * 16;
+    static constexpr uint32_t said = 8 * WARPS * kVoice + 8 * kFacts + kOwn;            // floats of an exchange
+    static constexpr uint32_t control = 3 * said * 4 + 128 + 3 * kNote * 4;
+    // of an entry of the teacher: index, logit, q and the student's logit, for three rows
+    static uint32_t smem(uint32_t top) { return 2 * bytes + control + top * 3 * 16 + table_slots(top) * 4; }
+};
+
+// The part of a row's 16-byte pieces that a CTA holds, and the single elements before and after the pieces.
+struct Part {
+    uint32_t head, pieces, begin, count;
+};
+
+template <typename T>
+__device__ __forceinline__ Part part_of(const T* row, uint32_t vocab, uint32_t rank, uint32_t ranks_log2) {
+    const uint32_t off = (uint32_t)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
+    Part p;
+    p.head = min(vocab, off ? kVec<T> - off : 0u);
+    p.pieces = (vocab - p.head) / kVec<T>;
+    p.begin = (uint32_t)(((uint64_t)p.pieces * rank) >> ranks_log2);
+    p.count = (uint32_t)(((uint64_t)p.pieces * (rank + 1)) >> ranks_log2) - p.begin;
+    return p;
+}
+
+// Which second exponential a row's logits have beside 2^((s - m) c_t): none, one of its own at c_1, or, at temperatures 2 and
+// 4, the first one's square or fourth power, which spares the unit that computes exponentials and is what bounds such rows.
+enum { kNoSecond = 0, kOwnSecond = 1, kSquare = 2, kFourth = 4 };
+
+template <int SECOND>
+__device__ __forceinline__ float power(float x) {
+    return SECOND == kFourth ? (x * x) * (x * x) : x * x;
+}
+template <int SECOND>
+__device__ __forceinline__ uint64_t power(uint64_t x) {
+    const uint64_t s = mul_pair(x, x);
+    return SECOND == kFourth ? mul_pair(s, s) : s;
+}
+
+// The exponent that a part with maximum m takes off its second exponentials.
+template <int SECOND>
+__device__ __forceinline__ float reference_1(float m, float c, float c_1) {
+    return SECOND == kOwnSecond ? reference(m, c_1) : SECOND * reference(m, c);
+}
+
+// The row's maximum and sums from what all dense warps of the cluster said.
+template <int SECOND>
+__device__ __forceinline__ void row_sums(const float* said, uint32_t voices, uint32_t lane, float c, float c_1, float& m,
+                                         float& sum_t, float& sum_1) {
+    m = -INFINITY;
+    for (uint32_t i = lane; i < voices; i += 32) m = fmaxf(m, said[i * kVoice + kMax]);
+    m = warp_max(m);
+    sum_t = sum_1 = 0.0f;
+    for (uint32_t i = lane; i < voices; i += 32) {
+        const float4 v = *reinterpret_cast<const float4*>(said + i * kVoice);
+        sum_t += v.y * rescale(v.x, m, c);
+        if (SECOND == kOwnSecond) sum_1 += v.z * rescale(v.x, m, c_1);
+        if (SECOND > kOwnSecond) sum_1 += v.z * power<SECOND>(rescale(v.x, m, c));
+    }
+    sum_t = warp_sum(sum_t);
+    sum_1 = SECOND ? warp_sum(sum_1) : sum_t;
+}
+
+// WARPS warps turn a slice into exponentials and these into the gradient; beside them one warp prepares the teacher's
+// entries and the label of a row, and one writes the loss and the entries' gradients and asks for the next slice.  They
+// meet at barriers in shared memory: `full` (a slice is there), `told` (an exchange is complete), `handed` (the
+// entries are prepared) and `done` (the dense result is stored).  Nothing else keeps them in step, so that the three kinds work on
+// different rows at a time.  SECOND: see kNoSecond.
+template <typename T, int WARPS, int PIECES, int CTAS, int SECOND>
+__global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(const T* logits, T* dlogits, const DistillArgs a) {
+    using S = SliceShape<T, WARPS, PIECES>;
+    constexpr int V = kVec<T>, kDense = 32 * WARPS;
+    extern __shared__ __align__(128) uint8_t smem[];
+    T* const slice = reinterpret_cast<T*>(smem);                                   // [2][pieces * V]
+    float* const exchange = reinterpret_cast<float*>(smem + 2 * S::bytes);         // [3][said]
+    const uint32_t bars = smem_addr(exchange + 3 * S::said);
+    float* const notes = exchange + 3 * S::said + 32;                              // [3][kNote]
+    int32_t* const all_idx = reinterpret_cast<int32_t*>(smem + 2 * S::bytes + S::control);   // [3][top] each
+    float* const all_t = reinterpret_cast<float*>(all_idx + 3 * a.top);
+    float* const all_q = all_t + 3 * a.top;
+    float* const all_z = all_q + 3 * a.top;
+    int32_t* const table = reinterpret_cast<int32_t*>(all_z + 3 * a.top);
+    auto full = [&](uint32_t turn) { return bars + 8 * (turn & 1u); };
+    auto done = [&](uint32_t turn) { return bars + 16 + 8 * (turn & 1u); };
+    auto handed = [&](uint32_t turn) { return bars + 32 + 8 * (turn & 1u); };
+    auto told = [&](uint32_t third) { return bars + 48 + 8 * third; };
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t ranks = cluster_size(), rank = cluster_rank(), ranks_log2 = __ffs(ranks) - 1;   // a power of two
+    const uint32_t first = blockIdx.x >> ranks_log2, step = gridDim.x >> ranks_log2;
+    const uint32_t voices = ranks * WARPS;
+    const float c_t = kLog2e / a.temperature, c_1 = kLog2e, c = a.kd != 0.0f ? c_t : c_1;
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(full(i), 1);
+            mbar_init(done(i), WARPS);
+            mbar_init(handed(i), 1);
+        }
+        for (int i = 0; i < 3; ++i) mbar_init(told(i), 1);
+        mbar_init_fence();
+    }
+    __syncthreads();
+    cluster_sync();             // every CTA of the cluster runs and has its barriers
+
+    bool ok = true;
+    uint32_t turn = 0, third = 0, thirds = 0;         // row `turn` exchanges through buffer `third` for the `thirds`-th time
+    if (warp < WARPS) {
+        for (uint64_t row = first; row < a.rows; row += step, ++turn) {
+            const T* const z = logits + row * a.ldl;
+            T* const out = dlogits ? dlogits + row * a.ldd : nullptr;
+            const Part p = part_of(z, a.vocab, rank, ranks_log2);
+            const T* const held = slice + (turn & 1u) * S::pieces * V;
+            const uint32_t tail = p.head + p.pieces * V, from = p.head + p.begin * V;
+            const bool head_mine = rank == 0 && tid < p.head, tail_mine = rank == ranks - 1 && tid < a.vocab - tail;
+            float single[2] = {-INFINITY, -INFINITY};                    // the thread's element of the head and of the tail
+            if (head_mine) single[0] = to_f32(z[tid]);
+            if (tail_mine) single[1] = to_f32(z[tail + tid]);
+            if (!(ok = mbar_wait(full(turn), (turn >> 1) & 1u))) break;
+            alignas(16) uint32_t raw[PIECES][4], most = Words<T>::lowest;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const uint32_t piece = i * kDense + tid;
+                uint4 q = make_uint4(Words<T>::lowest, Words<T>::lowest, Words<T>::lowest, Words<T>::lowest);
+                if (piece < p.count) q = *reinterpret_cast<const uint4*>(held + piece * V);
+                raw[i][0] = q.x, raw[i][1] = q.y, raw[i][2] = q.z, raw[i][3] = q.w;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) most = Words<T>::max(most, raw[i][u]);
+            }
+            const float m_w = warp_max(fmaxf(Words<T>::top(most), fmaxf(single[0], single[1])));
+            const float base = m_w == -INFINITY ? 0.0f : m_w;
+            const float off = fabsf(base) < kFar ? 0.0f : base;          // taken away first where m c does not fit
+            if (off != 0.0f)
+#pragma unroll 1
+                for (int i = 0; i < PIECES; ++i) {
+                    // back from shared memory: registers have no index.  The result is 0, or beyond any exponential
+                    const uint32_t piece = i * kDense + tid;
+                    float f[V];
+#pragma unroll
+                    for (int u = 0; u < V; ++u) f[u] = piece < p.count ? to_f32(held[piece * V + u]) - off : -INFINITY;
+                    alignas(16) uint32_t words[4];
+                    store_pack<T, V>(reinterpret_cast<T*>(words), f);
+#pragma unroll
+                    for (int j = 0; j < PIECES; ++j)
+                        if (j == i) raw[j][0] = words[0], raw[j][1] = words[1], raw[j][2] = words[2], raw[j][3] = words[3];
+                }
+            const uint64_t by2 = pair_of(c, c), k2 = pair_of(-reference(base, c), -reference(base, c));
+            uint64_t e[S::elems / 2], sum2 = pair_of(0.0f, 0.0f), other2 = sum2;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                for (int u = 0; u < V / 2; ++u) {
+                    float lo, hi;
+                    const uint64_t x = Words<T>::pair(raw[i], u);
+                    split_pair(fma_pair(x, by2, k2), lo, hi);
+                    e[i * (V / 2) + u] = pair_of(exp2_approx(lo), exp2_approx(hi));
+                    sum2 = add_pair(sum2, e[i * (V / 2) + u]);
+                    if constexpr (SECOND > kOwnSecond) other2 = add_pair(other2, power<SECOND>(e[i * (V / 2) + u]));
+                    if constexpr (SECOND == kOwnSecond) {
+                        split_pair(fma_pair(x, pair_of(c_1, c_1), pair_of(-reference(base, c_1), -reference(base, c_1))), lo, hi);
+                        other2 = add_pair(other2, pair_of(exp2_approx(lo), exp2_approx(hi)));
+                    }
+                }
+            float sum_t, sum_1 = 0.0f, lo, hi;
+            split_pair(sum2, lo, hi);
+            sum_t = lo + hi;
+            if constexpr (SECOND) {
+                split_pair(other2, lo, hi);
+                sum_1 = lo + hi;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if constexpr (SECOND == kOwnSecond) sum_1 += exp2_approx(fmaf(single[i] - off, c_1, -reference(base, c_1)));
+                single[i] = exp2_approx(fmaf(single[i] - off, c, -reference(base, c)));
+                if constexpr (SECOND > kOwnSecond) sum_1 += power<SECOND>(single[i]);
+                sum_t += single[i];
+            }
+            sum_t = warp_sum(sum_t);
+            if constexpr (SECOND) sum_1 = warp_sum(sum_1);
+            float* const said = exchange + third * S::said;
+            if (lane < ranks)
+                send_cluster(cluster_addr(smem_addr(said + (rank * WARPS + warp) * kVoice), lane), m_w, sum_t, sum_1, 0.0f,
+                             cluster_addr(told(third), lane));
+            if (!(ok = mbar_wait(told(third), thirds & 1u))) break;
+            float m;
+            row_sums<SECOND>(said, voices, lane, c, c_1, m, sum_t, sum_1);
+            const float* const own = said + 8 * WARPS * kVoice + 8 * kFacts;
+            if (++third == 3) third = 0, ++thirds;
+            if (out) {
+                const float coef_t = own[kCoefT], coef_1 = own[kCoef1];
+                // a row without a term, or with nothing but -inf, has gradient 0, whatever it holds
+                const bool none = sum_t == 0.0f || (coef_t == 0.0f && coef_1 == 0.0f);
+                // one factor takes what the registers hold to the gradient
+                const float up = rescale(m_w, m, c), g = (SECOND ? coef_t : coef_t + coef_1) / sum_t * up;
+                const float g_1 = SECOND ? coef_1 / sum_1 * (SECOND == kOwnSecond ? 1.0f : power<SECOND>(up)) : 0.0f;
+                const uint64_t g2 = pair_of(g, g), g2_1 = pair_of(g_1, g_1);
+                const float k_1 = SECOND ? -reference_1<SECOND>(m, c, c_1) : 0.0f, off_1 = fabsf(m) < kFar ? 0.0f : m;
+                // the second term, of a logit and its exponential
+                auto also = [&](float v, float x) {
+                    if (SECOND == kNoSecond) return 0.0f;
+                    return g_1 * (SECOND == kOwnSecond ? exp2_approx(fmaf(v - off_1, c_1, k_1)) : power<SECOND>(x));
+                };
+                const bool wide = ((reinterpret_cast<uintptr_t>(out + from)) & 15u) == 0;
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {
+                    const uint32_t piece = i * kDense + tid;
+                    if (piece < p.count) {
+                        float v[V];
+                        if constexpr (SECOND == kOwnSecond) unpack<T, V>(load_pack<T, V>(held + piece * V), v);
+#pragma unroll
+                        for (int u = 0; u < V / 2; ++u) {
+                            uint64_t x = e[i * (V / 2) + u];
+                            // its power is computed again: the first walk's would be kept in as many registers as e
+                            if constexpr (SECOND > kOwnSecond) asm volatile("" : "+l"(x));
+                            uint64_t r = mul_pair(g2, x);
+                            if constexpr (SECOND == kOwnSecond) r = add_pair(r, pair_of(also(v[2 * u], 0.0f), also(v[2 * u + 1], 0.0f)));
+                            if constexpr (SECOND > kOwnSecond) r = fma_pair(g2_1, power<SECOND>(x), r);
+                            split_pair(r, v[2 * u], v[2 * u + 1]);
+                        }
+                        if (none)
+#pragma unroll
+                            for (int u = 0; u < V; ++u) v[u] = 0.0f;
+                        T* const o = out + from + piece * V;
+                        if (wide) {
+                            store_pack<T, V>(o, v);
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < V; ++u) o[u] = from_f32<T>(v[u]);
+                        }
+                    }
+                }
+                if (head_mine) out[tid] = from_f32<T>(none ? 0.0f : g * single[0] + also(to_f32(z[tid]), single[0]));
+                if (tail_mine) out[tail + tid] = from_f32<T>(none ? 0.0f : g * single[1] + also(to_f32(z[tail + tid]), single[1]));
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(done(turn));
+        }
+    } else {
+        const uint32_t top = a.kd != 0.0f ? a.top : 0u;
+        const bool front = warp == WARPS;
+        auto request = [&](uint64_t row, uint32_t at) {
+            if (lane != 0 || row >= a.rows) return;
+            const T* const z = logits + row * a.ldl;
+            const Part p = part_of(z, a.vocab, rank, ranks_log2);
+            mbar_expect_tx(full(at), p.count * 16);
+            if (p.count) bulk_load(smem_addr(slice + (at & 1u) * S::pieces * V), z + p.head + (uint64_t)p.begin * V, p.count * 16, full(at));
+        };
+        const uint32_t slots = table_slots(a.top), table_shift = 32 - (__ffs(slots) - 1);
+        if (!front) {
+            request(first, 0);
+            request(first + (uint64_t)step, 1);
+            for (uint32_t s = lane; s < slots; s += 32) table[s] = -1;
+            __syncwarp();
+        }
+        // the first 64 entries of the next row travel through registers, further ones are read when they are needed
+        int32_t next_i[2] = {-1, -1}, next_y = -1;
+        float next_t[2] = {-INFINITY, -INFINITY}, next_w = 1.0f;
+        auto fetch = [&](uint64_t row) {
+            if (row >= a.rows) return;
+            if (front)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (u * 32 + lane < top) {
+                        next_i[u] = a.idx[row * a.top + u * 32 + lane];
+                        next_t[u] = load_teacher(a.teacher, a.teacher_type, row * a.top + u * 32 + lane);
+                    }
+            if (a.weight) next_w = __ldg(a.weight + row);
+            if (a.label) next_y = __ldg(a.label + row);
+        };
+        fetch(first);
+        for (uint64_t row = first; row < a.rows; row += step, ++turn) {
+            const T* const z = logits + row * a.ldl;
+            T* const out = dlogits ? dlogits + row * a.ldd : nullptr;
+            const Part p = part_of(z, a.vocab, rank, ranks_log2);
+            const uint32_t tail = p.head + p.pieces * V, from = p.head + p.begin * V, to = from + p.count * V;
+            auto mine = [&](uint32_t i) {
+                return (i >= from && i < to) || (rank == 0 && i < p.head) || (rank == ranks - 1 && i >= tail);
+            };
+            const float w = next_w;
+            const int32_t y = next_y;
+            const bool has_label = a.ce != 0.0f && y >= 0 && (uint32_t)y < a.vocab, label_mine = has_label && mine(y);
+            int32_t* const s_idx = all_idx + third * a.top;               // -1: not in this slice
+            float *const s_t = all_t + third * a.top, *const s_q = all_q + third * a.top, *const s_z = all_z + third * a.top;
+            float* const note = notes + third * kNote;
+            float* const said = exchange + third * S::said;
+            float* const facts = said + 8 * WARPS * kVoice;
+            if (front) {
+                // the slice's arrival also says that the entries of three rows ago are done with
+                if (!(ok = mbar_wait(full(turn), (turn >> 1) & 1u))) break;
+                const T* const held = slice + (turn & 1u) * S::pieces * V;
+                auto value = [&](uint32_t i) { return i >= from && i < to ? to_f32(held[i - from]) : to_f32(z[i]); };
+                const float z_label = label_mine ? value(y) : 0.0f;
+                // the teacher's softmax, and the logits at those of its entries that are in this slice
+                float tmax = -INFINITY, base = -INFINITY, total = 0.0f;
+                bool any = false;
+                for (uint32_t j = lane, u = 0; j < top; j += 32, ++u) {
+                    int32_t i = u == 0 ? next_i[0] : next_i[1];
+                    float t = u == 0 ? next_t[0] : next_t[1];
+                    if (u > 1) i = a.idx[row * a.top + j], t = load_teacher(a.teacher, a.teacher_type, row * a.top + j);
+                    const bool there = i >= 0 && (uint32_t)i < a.vocab, here = there && mine(i);
+                    if (!there) t = -INFINITY;
+                    const float v = here ? value(i) : -INFINITY;
+                    s_idx[j] = here ? i : -1;
+                    s_t[j] = t;
+                    s_z[j] = v;
+                    tmax = fmaxf(tmax, t);
+                    base = fmaxf(base, v);
+                    any |= t != -INFINITY;
+                }
+                fetch(row + step);
+                const bool has_teacher = __any_sync(0xFFFFFFFFu, any);
+                tmax = warp_max(tmax);
+                base = warp_max(base);
+                if (base == -INFINITY) base = 0.0f;
+                // sums over 2^((t - tmax) c): all entries', and of those in this slice also the terms of the loss
+                float sum_q = 0.0f, term = 0.0f;
+                for (uint32_t j = lane; j < top; j += 32) {
+                    const float t = s_t[j] - tmax, q = exp2_approx(t * c_t);
+                    s_q[j] = q;
+                    total += q;
+                    if (s_idx[j] >= 0 && q != 0.0f) {
+                        sum_q += q;
+                        term += q * (t - (s_z[j] - base));
+                    }
+                }
+                total = warp_sum(total), sum_q = warp_sum(sum_q), term = warp_sum(term);
+                const float per = 1.0f / total;
+                if (lane == 0) {
+                    mbar_expect_tx(told(third), voices * kVoice * 4 + kOwn * 4 + (rank == 0 ? ranks * kFacts * 4 : 0));
+                    send_cluster(cluster_addr(smem_addr(facts + 8 * kFacts), rank), has_teacher ? w * a.kd * a.temperature : 0.0f,
+                                 has_label ? w * a.ce : 0.0f, 0.0f, 0.0f, cluster_addr(told(third), rank));
+                    const uint32_t dst = cluster_addr(smem_addr(facts + rank * kFacts), 0), bar = cluster_addr(told(third), 0);
+                    send_cluster(dst, base, has_teacher ? sum_q * per : 0.0f, has_teacher ? term * per : 0.0f, label_mine ? 1.0f : 0.0f, bar);
+                    send_cluster(dst + 16, z_label, 0.0f, 0.0f, 0.0f, bar);
+                    note[kNoteTotal] = total;
+                    note[kNoteLabel] = z_label;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(handed(turn));
+                if (++third == 3) third = 0, ++thirds;
+                continue;
+            }
+            fetch(row + step);
+            if (!(ok = mbar_wait(handed(turn), (turn >> 1) & 1u))) break;
+            // entries that share an index: found by putting the indices into a table, and only then told apart
+            const float total = note[kNoteTotal];
+            bool shared = false;
+            if (out) {
+                for (uint32_t j = lane; j < top; j += 32) {
+                    const int32_t i = s_idx[j];
+                    if (i < 0) continue;
+                    uint32_t s = ((uint32_t)i * 2654435761u) >> table_shift;
+                    int32_t was;
+                    while ((was = atomicCAS(table + s, -1, i)) != -1 && was != i) s = (s + 1) & (slots - 1);
+                    shared |= was == i;
+                    s_t[j] = __uint_as_float(s);              // the teacher's logits are not needed any more
+                }
+                shared = __any_sync(0xFFFFFFFFu, shared);
+                for (uint32_t j = lane; j < top; j += 32) {
+                    const int32_t i = s_idx[j];
+                    if (i < 0) continue;
+                    table[__float_as_uint(s_t[j])] = -1;
+                    float q = s_q[j];
+                    bool leads = true;
+                    if (shared) {                             // the first of them stands for the sum
+                        q = 0.0f;
+                        for (uint32_t k = 0; k < top; ++k)
+                            if (s_idx[k] == i) {
+                                q += s_q[k];
+                                leads = leads && k >= j;
+                            }
+                    }
+                    s_t[j] = leads ? q / total : -1.0f;
+                }
+                __syncwarp();
+            }
+            if (!(ok = mbar_wait(told(third), thirds & 1u))) break;
+            float m, sum_t, sum_1;
+            row_sums<SECOND>(said, voices, lane, c, c_1, m, sum_t, sum_1);
+            const float coef_t = facts[8 * kFacts + kCoefT], coef_1 = facts[8 * kFacts + kCoef1];
+            const bool none = sum_t == 0.0f || (coef_t == 0.0f && coef_1 == 0.0f);
+            if (m == -INFINITY) m = 0.0f;
+            if (rank == 0) {
+                // s - base becomes s - m
+                float loss = 0.0f, q = 0.0f, part = 0.0f, label = 0.0f;
+                if (lane < ranks) {
+                    const float* const f = facts + lane * kFacts;
+                    q = f[kQ];
+                    part = f[kTerm] + (q != 0.0f ? q * (m - f[kBase]) : 0.0f);
+                    if (f[kHasLabel] != 0.0f) label = f[kLabel] - m;
+                }
+                q = warp_sum(q), part = warp_sum(part), label = warp_sum(label);
+                // T (log q - log p^T) with the temperature multiplied out: (s - m) / T would overflow for the lowest
+                // values that masks put in place of logits
+                if (coef_t != 0.0f) loss = a.kd * a.temperature * (part + q * a.temperature * (log_sum(sum_t, m, c) - logf(total)));
+                if (has_label) loss += a.ce * (log_sum(sum_1, m, SECOND == kOwnSecond ? c_1 : c, SECOND > kOwnSecond ? SECOND : 1) - label);
+                if (lane == 0) a.loss[row] = none ? 0.0f : w * loss;
+            }
+            if (++third == 3) third = 0, ++thirds;
+            // 2^((s - m) c) relative to the sums as they are kept
+            const float abs_t = (SECOND ? coef_t : coef_t + coef_1) / sum_t * exp2_approx(fabsf(m) < kFar ? fmaf(m, c, -ceilf(m * c)) : 0.0f);
+            const float abs_1 = SECOND ? coef_1 / sum_1 * exp2_approx(fabsf(m) < kFar ? fmaf(m, c_1, -reference_1<SECOND>(m, c, c_1)) : 0.0f) : 0.0f;
+            auto dense = [&](float v) {
+                const float d = abs_t * exp2_approx((v - m) * c);
+                return SECOND ? fmaf(abs_1, exp2_approx((v - m) * c_1), d) : d;
+            };
+            if (!(ok = mbar_wait(done(turn), (turn >> 1) & 1u))) break;
+            request(row + 2 * (uint64_t)step, turn);
+            if (out && !none) {
+                bool taken = false;      // the label is also an entry of the teacher
+                for (uint32_t j = lane; j < top; j += 32) {
+                    const int32_t i = s_idx[j];
+                    if (i < 0 || coef_t == 0.0f) continue;
+                    taken |= label_mine && i == y;
+                    if (s_t[j] == -1.0f) continue;
+                    out[i] = from_f32<T>(dense(s_z[j]) - coef_t * s_t[j] - (label_mine && i == y ? coef_1 : 0.0f));
+                }
+                taken = __any_sync(0xFFFFFFFFu, taken);
+                if (lane == 0 && label_mine && !taken) out[y] = from_f32<T>(dense(note[kNoteLabel]) - coef_1);
+            }
+            __syncwarp();
+        }
+    }
+    if (!ok) {
+        atomicExch(&g_distill_status, SLIMDP_ERR_INTERNAL);
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // copies under way end meanwhile
+    }
+    __syncthreads();
+    __syncwarp();
+    cluster_sync();
+}
+
+template <typename T, int WARPS, int PIECES, int CTAS, int SECOND>
+slimdp_status launch_slices(const T* logits, T* dlogits, const DistillArgs& a, uint32_t ranks, cudaStream_t st) {
+    using S = SliceShape<T, WARPS, PIECES>;
+    static DeviceOnce once;
+    auto kernel = distill_slice_kernel<T, WARPS, PIECES, CTAS, SECOND>;
+    if (once.needed()) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem(SLIMDP_MAX_TOP)) != cudaSuccess)
+            return SLIMDP_ERR_CUDA;
+        once.mark();
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ranks);
+    cfg.blockDim = dim3(32 * WARPS + 64);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    // as many clusters as run at once: one beyond them would start when the first ones have done their rows.  Lists of
+    // up to 256 entries take the shared memory of 256, longer ones that of the longest.
+    static std::atomic<int> resident[64][2][9];     // by device, list and ranks; 0 = not asked yet
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SLIMDP_ERR_CUDA;
+    const int list = a.top > 256;
+    cfg.dynamicSmemBytes = S::smem(list ? SLIMDP_MAX_TOP : 256);
+    int clusters = resident[dev][list][ranks].load(std::memory_order_relaxed);
+    if (clusters == 0) {
+        if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess || clusters <= 0) return SLIMDP_ERR_CUDA;
+        resident[dev][list][ranks].store(clusters, std::memory_order_relaxed);
+    }
+    cfg.gridDim = dim3(ranks * (unsigned)std::min<uint64_t>(a.rows, (uint64_t)clusters));
+    if (cudaLaunchKernelEx(&cfg, kernel, logits, dlogits, a) != cudaSuccess) return SLIMDP_ERR_CUDA;
+    SLIMDP_LAUNCHED(1);
+    return SLIMDP_OK;
+}
+
+template <typename T, int SECOND>
+slimdp_status launch_by_length(const T* z, T* d, const DistillArgs& a, uint64_t pieces, cudaStream_t st) {
+    if (pieces <= 256) return launch_slices<T, 2, 4, 8, SECOND>(z, d, a, 1, st);
+    for (uint32_t ranks = 1; ranks <= 8; ranks *= 2)
+        if (pieces <= (uint64_t)ranks * 2048) return launch_slices<T, 8, 8, 2, SECOND>(z, d, a, ranks, st);
+    return launch_slices<T, 16, 8, 1, SECOND>(z, d, a, 8, st);
+}
+
 }  // namespace
+
+slimdp_status read_distill_status() {
+    int status = 0;
+    return cudaMemcpyFromSymbol(&status, g_distill_status, sizeof(status)) == cudaSuccess ? status : SLIMDP_ERR_CUDA;
+}
 
 slimdp_status launch_distill(const void* logits, uint64_t ldl, uint32_t rows, uint32_t vocab, int32_t type,
                              const int32_t* idx, const void* teacher, int32_t teacher_type, uint32_t top,
@@ -259,6 +850,16 @@ slimdp_status launch_distill(const void* logits, uint64_t ldl, uint32_t rows, ui
     const DistillArgs a = {ldl, ldd, rows, vocab, top, idx, teacher, teacher_type, label, weight, temperature, kd, ce, loss};
     return with_type(type, [&](auto e) -> slimdp_status {
         using T = decltype(e);
+        // 16-byte pieces of a row, and the fewest CTAs of a cluster whose slices hold them
+        const uint64_t pieces = (uint64_t)vocab / kVec<T>;
+        const T* const z = (const T*)logits;
+        T* const d = (T*)dlogits;
+        if (pieces <= 8 * 4096) {
+            if (kd == 0.0f || ce == 0.0f || temperature == 1.0f) return launch_by_length<T, kNoSecond>(z, d, a, pieces, st);
+            if (temperature == 2.0f) return launch_by_length<T, kSquare>(z, d, a, pieces, st);
+            if (temperature == 4.0f) return launch_by_length<T, kFourth>(z, d, a, pieces, st);
+            return launch_by_length<T, kOwnSecond>(z, d, a, pieces, st);
+        }
         distill_kernel<T><<<rows, kDistillThreads, 0, st>>>((const T*)logits, (T*)dlogits, a);
         SLIMDP_LAUNCHED(1);
         return SLIMDP_OK;

@@ -616,11 +616,9 @@ size_t linear_ws_bytes(uint64_t m, uint64_t n, uint64_t k, int32_t type) {
     return 256 + std::max({x + w + partial(m, n, k), dy + w + partial(m, k, n), dy + x + partial(n, k, m)});
 }
 
-slimdp_status read_product_status(cudaStream_t st) {
+slimdp_status read_product_status() {
     int status = 0;
-    if (cudaStreamSynchronize(st) != cudaSuccess || cudaMemcpyFromSymbol(&status, g_product_status, sizeof(status)) != cudaSuccess)
-        return SLIMDP_ERR_CUDA;
-    return status;
+    return cudaMemcpyFromSymbol(&status, g_product_status, sizeof(status)) == cudaSuccess ? status : SLIMDP_ERR_CUDA;
 }
 
 slimdp_status launch_linear_forward(const void* x, uint64_t ldx, const void* w, uint64_t ldw, const float* bias,

@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace slimdp {
@@ -52,12 +54,28 @@ __device__ __forceinline__ void unpack(const Pack<T, N>& p, float* f) {
     for (int i = 0; i < N; ++i) f[i] = to_f32(p.v[i]);
 }
 
+// Two values rounded and packed by one instruction.
+template <typename T>
+__device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 r = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&r);
+    } else {
+        const __nv_bfloat162 r = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&r);
+    }
+}
+
 template <typename T, int N>
 __device__ __forceinline__ void store_pack(T* p, const float* f) {
-    Pack<T, N> r;
+    if constexpr (sizeof(T) == 2 && N == 8) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_two<T>(f[0], f[1]), pack_two<T>(f[2], f[3]), pack_two<T>(f[4], f[5]), pack_two<T>(f[6], f[7]));
+    } else {
+        Pack<T, N> r;
 #pragma unroll
-    for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(f[i]);
-    *reinterpret_cast<Pack<T, N>*>(p) = r;
+        for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(f[i]);
+        *reinterpret_cast<Pack<T, N>*>(p) = r;
+    }
 }
 
 // Elements of a 16-byte access.
@@ -76,9 +94,9 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 __device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
-    return v;
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 // 2^x; the hardware's approximation (2 ulp, subnormal results to 0) is below the rounding of what is made of it.

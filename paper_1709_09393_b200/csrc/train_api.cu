@@ -29,7 +29,8 @@ slimdp_status launch_linear_backward_weight(const void* dy, uint64_t lddy, const
 slimdp_status launch_activation_backward(const void* dy, uint64_t lddy, const void* z, uint64_t ldz, uint64_t m,
                                          uint64_t n, int32_t type, int32_t act, void* dz, uint64_t lddz,
                                          cudaStream_t st);
-slimdp_status read_product_status(cudaStream_t st);
+slimdp_status read_product_status();
+slimdp_status read_distill_status();
 slimdp_status launch_distill(const void* logits, uint64_t ldl, uint32_t rows, uint32_t vocab, int32_t type,
                              const int32_t* idx, const void* teacher, int32_t teacher_type, uint32_t top,
                              const int32_t* label, const float* weight, float temperature, float kd, float ce,
@@ -161,7 +162,11 @@ slimdp_status slimdp_activation_backward(const void* dy, uint64_t lddy, const vo
     return launch_activation_backward(dy, lddy, z, ldz, m, n, type, act, dz, lddz, (cudaStream_t)stream);
 }
 
-slimdp_status slimdp_linear_read_status(void* stream) { return read_product_status((cudaStream_t)stream); }
+slimdp_status slimdp_train_read_status(void* stream) {
+    if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return SLIMDP_ERR_CUDA;
+    const slimdp_status s = read_product_status();
+    return s != SLIMDP_OK ? s : read_distill_status();
+}
 
 slimdp_status slimdp_distill(const void* logits, uint64_t ldl, uint64_t rows, uint64_t vocab, int32_t type,
                              const int32_t* teacher_idx, const void* teacher_logit, int32_t teacher_type, uint32_t top,

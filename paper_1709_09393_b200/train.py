@@ -163,9 +163,9 @@ def slimdp_linear_backward_weight(dy: torch.Tensor, x: torch.Tensor, dw: torch.T
                                               bool(accumulate), pws, nws, _stream(stream)))
 
 
-def linear_read_status(stream=None) -> None:
-    """Synchronises, and raises if a bounded wait of a product kernel ever ran out on this device."""
-    _check("slimdp_linear_read_status", _lib.slimdp_linear_read_status(_stream(stream)))
+def train_read_status(stream=None) -> None:
+    """Synchronises, and raises if a bounded wait of one of these kernels ever ran out on this device."""
+    _check("slimdp_train_read_status", _lib.slimdp_train_read_status(_stream(stream)))
 
 
 def slimdp_activation_backward(dy: torch.Tensor, z: torch.Tensor, dz: torch.Tensor, activation: str, stream=None):

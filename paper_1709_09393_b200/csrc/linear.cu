@@ -29,38 +29,55 @@ struct Epilogue {
 
 enum Product { kForward, kInput, kWeight };
 
+// What the epilogue reads at V adjacent results: loaded for several places at once, before any of them is worked on.
+template <typename T, Product P, int V>
+struct Extra {
+    Pack<T, V> z, add;
+    Pack<float, V> old;
+
+    __device__ __forceinline__ void load(const Epilogue& e, uint64_t i, uint64_t j) {
+        if constexpr (P == kInput)
+            if (e.act != SLIMDP_ACT_NONE) z = load_pack<T, V>((const T*)e.z + i * e.ldz + j);
+        if constexpr (P == kWeight) {
+            if (e.accumulate) old = load_pack<float, V>((const float*)e.out + i * e.ldo + j);
+        } else {
+            if (e.add) add = load_pack<T, V>((const T*)e.add + i * e.ldadd + j);
+        }
+    }
+};
+
 // V adjacent results C[i, j .. j + V), through the epilogue of product P; bias: the V values of these columns.
 template <typename T, Product P, int V>
-__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint64_t j, float (&v)[V], const float (&bias)[V]) {
+__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint64_t j, float (&v)[V], const float (&bias)[V],
+                                       const Extra<T, P, V>& x) {
     if constexpr (P == kForward) {
 #pragma unroll
         for (int c = 0; c < V; ++c) v[c] += bias[c];
         if (e.z) store_pack<T, V>((T*)e.z + i * e.ldz + j, v);
-        if (e.act != SLIMDP_ACT_NONE) {
+        with_act(e.act, [&](auto act) {
 #pragma unroll
-            for (int c = 0; c < V; ++c) v[c] = act_value(v[c], e.act);
-        }
+            for (int c = 0; c < V; ++c) v[c] = act_value<decltype(act)::value>(v[c]);
+        });
     } else if constexpr (P == kInput) {
-        if (e.act != SLIMDP_ACT_NONE) {
+        with_act(e.act, [&](auto act) {
             float z[V];
-            unpack<T, V>(load_pack<T, V>((const T*)e.z + i * e.ldz + j), z);
+            unpack<T, V>(x.z, z);
 #pragma unroll
-            for (int c = 0; c < V; ++c) v[c] *= act_slope(z[c], e.act);
-        }
+            for (int c = 0; c < V; ++c) v[c] *= act_slope<decltype(act)::value>(z[c]);
+        });
     }
     if constexpr (P == kWeight) {
-        float* o = (float*)e.out + i * e.ldo + j;
         if (e.accumulate) {
             float old[V];
-            unpack<float, V>(load_pack<float, V>(o), old);
+            unpack<float, V>(x.old, old);
 #pragma unroll
             for (int c = 0; c < V; ++c) v[c] += old[c];
         }
-        store_pack<float, V>(o, v);
+        store_pack<float, V>((float*)e.out + i * e.ldo + j, v);
     } else {
         if (e.add) {
             float a[V];
-            unpack<T, V>(load_pack<T, V>((const T*)e.add + i * e.ldadd + j), a);
+            unpack<T, V>(x.add, a);
 #pragma unroll
             for (int c = 0; c < V; ++c) v[c] += a[c];
         }
@@ -91,43 +108,61 @@ struct ProductArgs {
     Epilogue e;
 };
 
-// V results of one row, or as many as the row has left.
+// The last columns of a matrix whose width is not a multiple of V, one by one.
 template <typename T, Product P, int V>
-__device__ __forceinline__ void finish_columns(const ProductArgs& args, uint64_t i, uint64_t j, float (&v)[V]) {
-    const float* bias = P == kForward ? args.e.bias : nullptr;
-    if (j + V <= args.n) {
-        float b[V];
+__device__ __forceinline__ void finish_rest(const ProductArgs& args, uint64_t i, uint64_t j, const float (&v)[V]) {
 #pragma unroll
-        for (int c = 0; c < V; ++c) b[c] = bias ? __ldg(bias + j + c) : 0.0f;
-        finish<T, P, V>(args.e, i, j, v, b);
-    } else {
-#pragma unroll
-        for (int c = 0; c < V; ++c)
-            if (j + c < args.n) {
-                float one[1] = {v[c]}, b[1] = {bias ? __ldg(bias + j + c) : 0.0f};
-                finish<T, P, 1>(args.e, i, j + c, one, b);
-            }
-    }
+    for (int c = 0; c < V; ++c)
+        if (j + c < args.n) {
+            float one[1] = {v[c]}, b[1] = {P == kForward && args.e.bias ? __ldg(args.e.bias + j + c) : 0.0f};
+            Extra<T, P, 1> x;
+            x.load(args.e, i, j + c);
+            finish<T, P, 1>(args.e, i, j + c, one, b, x);
+        }
 }
 
 // A warp's 32 x 32 results, row-wise in shared memory: V adjacent columns a lane, so that a warp's accesses to memory
-// cover whole rows of the square.
+// cover whole rows of the square; what the epilogue reads for BATCH such accesses is asked for at once.
 template <typename T, Product P, int V, bool PARTIAL>
 __device__ __forceinline__ void finish_square_by(const ProductArgs& args, uint32_t split, const float* square,
                                                  uint64_t row0, uint64_t col0, uint32_t lane) {
+    constexpr int BATCH = V == 1 ? 8 : 4;
     const uint32_t c = lane % (32 / V) * V, r = lane / (32 / V);
-    if (col0 + c >= args.n) return;
-#pragma unroll 1
-    for (uint32_t r0 = r; r0 < 32; r0 += V) {
-        const uint64_t i = row0 + r0;
-        if (i >= args.m) break;
-        float v[V];
+    const uint64_t j = col0 + c;
+    if (j >= args.n || row0 >= args.m) return;
+    const uint32_t rows = (uint32_t)min((uint64_t)32, args.m - row0);
+    if constexpr (PARTIAL) {
+        for (uint32_t k = r; k < rows; k += V) {
+            float v[V];
 #pragma unroll
-        for (int u = 0; u < V; ++u) v[u] = square[r0 * kEpiloguePitch + c + u];
-        if constexpr (PARTIAL)
-            store_pack<float, V>(args.partial + ((uint64_t)split * args.m + i) * args.ld_partial + col0 + c, v);
-        else
-            finish_columns<T, P, V>(args, i, col0 + c, v);
+            for (int u = 0; u < V; ++u) v[u] = square[k * kEpiloguePitch + c + u];
+            store_pack<float, V>(args.partial + ((uint64_t)split * args.m + row0 + k) * args.ld_partial + j, v);
+        }
+    } else {
+        float bias[V];
+#pragma unroll
+        for (int u = 0; u < V; ++u) bias[u] = P == kForward && args.e.bias && j + u < args.n ? __ldg(args.e.bias + j + u) : 0.0f;
+        const bool whole = j + V <= args.n;
+#pragma unroll 1
+        for (uint32_t k0 = r; k0 < rows; k0 += V * BATCH) {
+            Extra<T, P, V> x[BATCH];
+            if (whole)
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b)
+                    if (k0 + b * V < rows) x[b].load(args.e, row0 + k0 + b * V, j);
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const uint32_t k = k0 + b * V;
+                if (k >= rows) break;
+                float v[V];
+#pragma unroll
+                for (int u = 0; u < V; ++u) v[u] = square[k * kEpiloguePitch + c + u];
+                if (whole)
+                    finish<T, P, V>(args.e, row0 + k, j, v, bias, x[b]);
+                else
+                    finish_rest<T, P, V>(args, row0 + k, j, v);
+            }
+        }
     }
 }
 
@@ -374,25 +409,75 @@ __global__ void __launch_bounds__(256) join_kernel(const ProductArgs args) {
 #pragma unroll
             for (int c = 0; c < V; ++c) v[c] += src[c];       // ld_partial is a multiple of V: in bounds
         }
-        finish_columns<T, P, V>(args, i, j, v);
+        if (j + V > args.n) {
+            finish_rest<T, P, V>(args, i, j, v);
+            continue;
+        }
+        float bias[V];
+#pragma unroll
+        for (int c = 0; c < V; ++c) bias[c] = P == kForward && args.e.bias ? __ldg(args.e.bias + j + c) : 0.0f;
+        Extra<T, P, V> x;
+        x.load(args.e, i, j);
+        finish<T, P, V>(args.e, i, j, v, bias, x);
     }
 }
 
-// db (+)= sum over rows of dy: a CTA takes 32 columns, its 32 warps every 32nd row each.
-template <typename T>
-__global__ void __launch_bounds__(1024) column_sum_kernel(const T* __restrict__ dy, uint64_t lddy, uint64_t m,
-                                                          uint64_t n, float* __restrict__ db, bool accumulate) {
-    __shared__ float smem[32][33];
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint64_t j = (uint64_t)blockIdx.x * 32 + lane;
-    float s = 0.0f;
-    if (j < n)
-        for (uint64_t i = warp; i < m; i += 32) s += to_f32(dy[i * lddy + j]);
-    smem[warp][lane] = s;
+// db (+)= sum over rows of dy.  A cluster of eight CTAs takes 32 V columns, each of its 128 warps every 128th row; sums go from
+// registers to shared memory to rank 0, in a fixed order.  Bound by reading dy: sixteen warps with four 16-byte loads a
+// thread in flight keep an SM's share of the bandwidth busy.
+constexpr uint32_t kSumRanks = 8, kSumWarps = 16;
+
+template <typename T, int V>
+__global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWarps)
+    column_sum_kernel(const T* __restrict__ dy, uint64_t lddy, uint64_t m, uint64_t n, float* __restrict__ db, bool accumulate) {
+    __shared__ float smem[kSumWarps][32 * V];
+    __shared__ float total[32 * V];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = cluster_rank();
+    const uint64_t j0 = (uint64_t)(blockIdx.x / kSumRanks) * 32 * V, j = j0 + lane * V;
+    const uint64_t stride = kSumRanks * kSumWarps;
+    float s[V] = {};
+    if (j + V <= n) {
+        uint64_t i = rank * kSumWarps + warp;
+        for (; i + 3 * stride < m; i += 4 * stride) {
+            Pack<T, V> p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) p[u] = load_pack<T, V>(dy + (i + u * stride) * lddy + j);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float f[V];
+                unpack<T, V>(p[u], f);
+#pragma unroll
+                for (int c = 0; c < V; ++c) s[c] += f[c];
+            }
+        }
+        for (; i < m; i += stride)
+#pragma unroll
+            for (int c = 0; c < V; ++c) s[c] += to_f32(dy[i * lddy + j + c]);
+    } else {
+        for (uint64_t i = rank * kSumWarps + warp; i < m; i += stride)
+#pragma unroll
+            for (int c = 0; c < V; ++c)
+                if (j + c < n) s[c] += to_f32(dy[i * lddy + j + c]);
+    }
+#pragma unroll
+    for (int c = 0; c < V; ++c) smem[warp][c * 32 + lane] = s[c];
     __syncthreads();
-    s = warp_sum(smem[lane][warp]);
-    const uint64_t c = (uint64_t)blockIdx.x * 32 + warp;
-    if (lane == 0 && c < n) db[c] = accumulate ? db[c] + s : s;
+    for (uint32_t c = threadIdx.x; c < 32 * V; c += 32 * kSumWarps) {
+        float t = 0.0f;
+#pragma unroll
+        for (uint32_t w = 0; w < kSumWarps; ++w) t += smem[w][c];
+        total[c] = t;
+    }
+    cluster_sync();
+    if (rank == 0)
+        for (uint32_t c = threadIdx.x; c < 32 * V; c += 32 * kSumWarps) {
+            const uint64_t col = j0 + (c & 31) * V + c / 32;
+            if (col >= n) continue;
+            float t = 0.0f;
+            for (uint32_t r = 0; r < kSumRanks; ++r) t += load_cluster(cluster_addr(smem_addr(total + c), r));
+            db[col] = accumulate ? db[col] + t : t;
+        }
+    cluster_sync();             // no CTA leaves while its sums are read
 }
 
 template <typename T>
@@ -403,7 +488,9 @@ __global__ void __launch_bounds__(256) activation_backward_kernel(const T* __res
     for (uint64_t i = blockIdx.y; i < m; i += gridDim.y)
         for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < n; j += (uint64_t)gridDim.x * 256) {
             const float d = to_f32(dy[i * lddy + j]);
-            dz[i * lddz + j] = from_f32<T>(act == SLIMDP_ACT_NONE ? d : d * act_slope(to_f32(z[i * ldz + j]), act));
+            float slope = 1.0f;
+            with_act(act, [&](auto a) { slope = act_slope<decltype(a)::value>(to_f32(z[i * ldz + j])); });
+            dz[i * lddz + j] = from_f32<T>(d * slope);
         }
 }
 
@@ -414,31 +501,56 @@ struct Matrix {
     uint64_t ld, rows, cols;
 };
 
-// Operands that TMA cannot read in place: rows that do not start on 16-byte boundaries are copied to rows that do.
-template <typename T>
-__global__ void __launch_bounds__(256) align_kernel(const T* __restrict__ src, uint64_t ld, uint64_t rows, uint64_t cols,
-                                                    T* __restrict__ dst, uint64_t ld_dst) {
-    for (uint64_t i = blockIdx.y; i < rows; i += gridDim.y)
-        for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < cols; j += (uint64_t)gridDim.x * 256)
-            dst[i * ld_dst + j] = src[i * ld + j];
+// fp32 = three bf16 parts, each the leading eight bits of what the ones before leave: cut, not rounded, so that no part
+// of a finite number overflows; the parts of a number that is not finite are itself and zeros.
+__device__ __forceinline__ void cut(float v, float (&part)[3]) {
+    const bool finite = fabsf(v) <= 3.4028234663852886e38f;
+    part[0] = finite ? __uint_as_float(__float_as_uint(v) & 0xFFFF0000u) : v;
+    const float r = finite ? v - part[0] : 0.0f;
+    part[1] = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
+    part[2] = r - part[1];                     // eight bits are left: exact in bf16
 }
 
-// fp32 = three bf16 parts, each the leading eight bits of what the ones before leave: cut, not rounded, so that no part
-// of a finite number overflows; the parts of a number without a finite leading part are that part and zeros.
-__global__ void __launch_bounds__(256) parts_kernel(const float* __restrict__ src, uint64_t ld, uint64_t rows, uint64_t cols,
-                                                    __nv_bfloat16* __restrict__ dst, uint64_t ld_dst) {
-    for (uint64_t i = blockIdx.y; i < rows; i += gridDim.y)
-        for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < cols; j += (uint64_t)gridDim.x * 256) {
-            float v = src[i * ld + j];
+// Brings up to two operands into a form that TMA reads: rows on 16-byte boundaries, fp32 as planes of parts.  Bound by memory (fp32:
+// 4 bytes read and 6 written an element); a thread takes eight adjacent elements, read 16 bytes at a time where the rows allow.
+struct PackJob {
+    const void* src;
+    void* dst;
+    uint64_t ld, ld_dst, rows, cols;
+    bool wide;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256) pack_kernel(PackJob job0, PackJob job1) {
+    const PackJob job = blockIdx.y ? job1 : job0;
+    const uint64_t groups = (job.cols + 7) / 8, total = groups * job.rows;
+    for (uint64_t g = (uint64_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (uint64_t)gridDim.x * 256) {
+        const uint64_t i = g / groups, j = (g - i * groups) * 8;
+        const T* const src = (const T*)job.src + i * job.ld + j;
+        T v[8];
+        if (job.wide && j + 8 <= job.cols) {
+#pragma unroll
+            for (int u = 0; u < 8; u += kVec<T>) *reinterpret_cast<Pack<T, kVec<T>>*>(v + u) = load_pack<T, kVec<T>>(src + u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = j + u < job.cols ? src[u] : T(0.0f);
+        }
+        // ld_dst is a multiple of eight: whole groups fit
+        if constexpr (sizeof(T) == 4) {
+            float part[8][3];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) cut(v[u], part[u]);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                const float head = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
-                const bool finite = fabsf(v) <= 3.4028234663852886e38f;
-                __nv_bfloat16 h = finite ? (p < 2 ? __float2bfloat16_rz(head) : __float2bfloat16_rn(v)) : __float2bfloat16_rn(v);
-                dst[((uint64_t)p * rows + i) * ld_dst + j] = h;
-                v = finite ? v - __bfloat162float(h) : 0.0f;
+                float f[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) f[u] = part[u][p];
+                store_pack<__nv_bfloat16, 8>((__nv_bfloat16*)job.dst + ((uint64_t)p * job.rows + i) * job.ld_dst + j, f);
             }
+        } else {
+            *reinterpret_cast<Pack<T, 8>*>((T*)job.dst + i * job.ld_dst + j) = *reinterpret_cast<Pack<T, 8>*>(v);
         }
+    }
 }
 
 uint64_t packed_ld(uint64_t cols) { return align_up(cols, 8); }
@@ -484,21 +596,29 @@ struct Scratch {
     }
 };
 
-// Brings an operand into a form that TMA reads: in place where its rows start on 16-byte boundaries.
+// Operands that TMA cannot read in place (fp32, or rows that do not start on 16-byte boundaries) are packed into scratch.
 template <typename T>
-slimdp_status prepare_operand(Matrix& a, Scratch& ws, cudaStream_t st) {
+slimdp_status prepare_operands(Matrix& a, Matrix& b, Scratch& ws, cudaStream_t st) {
     constexpr bool kSplit = sizeof(T) == 4;
-    if (!kSplit && aligned16(a.p) && a.ld % 8 == 0) return SLIMDP_OK;
-    const uint64_t ld = packed_ld(a.cols);
-    void* dst = ws.take(packed_bytes(a.rows, a.cols, kSplit ? SLIMDP_F32 : SLIMDP_BF16));
-    const dim3 grid((unsigned)std::min<uint64_t>((a.cols + 255) / 256, 64), (unsigned)std::min<uint64_t>(a.rows, 16384));
-    if constexpr (kSplit)
-        parts_kernel<<<grid, 256, 0, st>>>((const float*)a.p, a.ld, a.rows, a.cols, (__nv_bfloat16*)dst, ld);
-    else
-        align_kernel<T><<<grid, 256, 0, st>>>((const T*)a.p, a.ld, a.rows, a.cols, (T*)dst, ld);
+    PackJob job[2] = {};
+    int jobs = 0;
+    uint64_t most = 0;
+    for (Matrix* x : {&a, &b}) {
+        const bool wide = aligned16(x->p) && (x->ld * sizeof(T)) % 16 == 0;
+        if (!kSplit && wide) continue;
+        const uint64_t ld = packed_ld(x->cols);
+        void* dst = ws.take(packed_bytes(x->rows, x->cols, kSplit ? SLIMDP_F32 : SLIMDP_BF16));
+        job[jobs++] = {x->p, dst, x->ld, ld, x->rows, x->cols, wide};
+        most = std::max(most, x->rows * (ld / 8));
+        x->p = dst;
+        x->ld = ld;
+    }
+    if (jobs == 0) return SLIMDP_OK;
+    const int sms = sm_count();
+    if (sms <= 0) return SLIMDP_ERR_CUDA;
+    const dim3 grid((unsigned)std::min<uint64_t>((most + 255) / 256, (uint64_t)sms * 8), jobs);
+    pack_kernel<T><<<grid, 256, 0, st>>>(job[0], job[1]);
     SLIMDP_LAUNCHED(1);
-    a.p = dst;
-    a.ld = ld;
     return SLIMDP_OK;
 }
 
@@ -558,8 +678,7 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
                              cudaStream_t st) {
     constexpr bool kMnA = P == kWeight, kMnB = P != kForward, kF16 = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value;
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-    slimdp_status s = prepare_operand<T>(a, ws, st);
-    if (s == SLIMDP_OK) s = prepare_operand<T>(b, ws, st);
+    slimdp_status s = prepare_operands<T>(a, b, ws, st);
     if (s != SLIMDP_OK) return s;
     ProductArgs args = {};
     args.m = m;
@@ -653,7 +772,13 @@ slimdp_status launch_linear_backward_weight(const void* dy, uint64_t lddy, const
     return with_type(type, [&](auto v) -> slimdp_status {
         using T = decltype(v);
         if (db) {
-            column_sum_kernel<T><<<(unsigned)((n + 31) / 32), 1024, 0, st>>>((const T*)dy, lddy, m, n, db, accumulate);
+            const bool wide = aligned16(dy) && (lddy * sizeof(T)) % 16 == 0;
+            const uint64_t columns = wide ? 32 * kVec<T> : 32;
+            const unsigned ctas = (unsigned)((n + columns - 1) / columns) * kSumRanks;
+            if (wide)
+                column_sum_kernel<T, kVec<T>><<<ctas, 32 * kSumWarps, 0, st>>>((const T*)dy, lddy, m, n, db, accumulate);
+            else
+                column_sum_kernel<T, 1><<<ctas, 32 * kSumWarps, 0, st>>>((const T*)dy, lddy, m, n, db, accumulate);
             SLIMDP_LAUNCHED(1);
         }
         if (m == 0)

@@ -108,6 +108,12 @@ __device__ __forceinline__ void send_cluster(uint32_t addr, float a, float b, fl
                  : "memory");
 }
 
+__device__ __forceinline__ float load_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 __device__ __forceinline__ uint32_t cluster_size() {
     uint32_t r;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));

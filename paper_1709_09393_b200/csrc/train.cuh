@@ -108,36 +108,72 @@ __device__ __forceinline__ float exp2_approx(float x) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// z -> act(z).
-__device__ __forceinline__ float act_value(float z, int act) {
-    switch (act) {
-        case SLIMDP_ACT_RELU: return z != z ? z : fmaxf(z, 0.0f);
-        case SLIMDP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-        case SLIMDP_ACT_GELU_TANH: {
-            const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
-            return 0.5f * z * (1.0f + tanhf(u));
-        }
-        case SLIMDP_ACT_SILU: return z / (1.0f + expf(-z));
-        default: return z;
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The normal distribution's Phi(z) and phi(z) from one exponential: erfc(x) = p(t) exp(-x^2), t = 1 / (1 + 0.3275911 x), p of
+// degree 5, within 1.5e-7 (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26).  The lower tail is p(t) exp(-x^2) / 2
+// itself, without a difference from 1.
+__device__ __forceinline__ void normal(float z, float& cdf, float& pdf) {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = rcp_approx(fmaf(0.3275911f, x, 1.0f));
+    const float e = exp2_approx(x * x * -kLog2e);
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float tail = 0.5f * p * t * e;
+    cdf = z < 0.0f ? tail : 1.0f - tail;
+    pdf = 0.39894228040143268f * e;
+}
+
+__device__ __forceinline__ float logistic(float z) { return rcp_approx(1.0f + exp2_approx(z * -kLog2e)); }
+
+// z -> act(z).  0.5 (1 + tanh u) is logistic(2 u).
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == SLIMDP_ACT_RELU) return z != z ? z : fmaxf(z, 0.0f);
+    if constexpr (ACT == SLIMDP_ACT_GELU) {
+        float cdf, pdf;
+        normal(z, cdf, pdf);
+        return z * cdf;
     }
+    if constexpr (ACT == SLIMDP_ACT_GELU_TANH) return z * logistic(1.5957691216057308f * (z + 0.044715f * z * z * z));
+    if constexpr (ACT == SLIMDP_ACT_SILU) return z * logistic(z);
+    return z;
 }
 
 // z -> d act(z) / dz.
-__device__ __forceinline__ float act_slope(float z, int act) {
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == SLIMDP_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == SLIMDP_ACT_GELU) {
+        float cdf, pdf;
+        normal(z, cdf, pdf);
+        return fmaf(z, pdf, cdf);
+    }
+    if constexpr (ACT == SLIMDP_ACT_GELU_TANH) {
+        const float z2 = z * z, s = logistic(1.5957691216057308f * z * fmaf(0.044715f, z2, 1.0f));
+        return fmaf(s * (1.0f - s) * 1.5957691216057308f * z, fmaf(0.134145f, z2, 1.0f), s);
+    }
+    if constexpr (ACT == SLIMDP_ACT_SILU) {
+        const float s = logistic(z);
+        return fmaf(z * s, 1.0f - s, s);
+    }
+    return 1.0f;
+}
+
+// Calls f with the activation that `act` names as a constant; not for none.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
     switch (act) {
-        case SLIMDP_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-        case SLIMDP_ACT_GELU:
-            return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
-        case SLIMDP_ACT_GELU_TANH: {
-            const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
-            const float t = tanhf(u);
-            return 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * 0.79788456080286536f * (1.0f + 0.134145f * z * z);
-        }
-        case SLIMDP_ACT_SILU: {
-            const float s = 1.0f / (1.0f + expf(-z));
-            return s * (1.0f + z * (1.0f - s));
-        }
-        default: return 1.0f;
+        case SLIMDP_ACT_RELU: f(std::integral_constant<int, SLIMDP_ACT_RELU>()); break;
+        case SLIMDP_ACT_GELU: f(std::integral_constant<int, SLIMDP_ACT_GELU>()); break;
+        case SLIMDP_ACT_GELU_TANH: f(std::integral_constant<int, SLIMDP_ACT_GELU_TANH>()); break;
+        case SLIMDP_ACT_SILU: f(std::integral_constant<int, SLIMDP_ACT_SILU>()); break;
     }
 }
 

@@ -609,7 +609,7 @@ slimdp_status slimdp_distill(const void* logits, uint64_t ldl, uint64_t rows, ui
                              const int32_t* label, const float* row_weight, float temperature, float kd_weight,
                              float ce_weight, float* loss, void* dlogits, uint64_t ldd, void* stream);
 
-/* The waits of the product and distillation kernels are bounded (two seconds).  Synchronises `stream`, then returns SLIMDP_ERR_INTERNAL if one
+/* The waits of the kernels of a local step are bounded (two seconds).  Synchronises `stream`, then returns SLIMDP_ERR_INTERNAL if one
  * ever ran out on this device, SLIMDP_OK otherwise. */
 slimdp_status slimdp_train_read_status(void* stream);
 

@@ -4,106 +4,150 @@
 // y = (x - mean) rstd gamma + beta.  Backward with h = (x - mean) rstd and g = dy gamma:
 // dx = rstd (g - avg(g) - h avg(g h)), dgamma = sum over rows of dy h, dbeta = sum over rows of dy.
 //
-// Both directions are bound by memory: each element is read once and written once, so a row stays in
-// registers between its reductions and its result.  A group of threads (a warp for rows of up to 1024 elements, a
-// CTA beyond) owns fixed columns and walks over rows; gamma, beta and the column sums of the gradients stay in
-// registers all the while.  The variance is summed about the mean (a second reduction over registers, no
-// second pass over memory), so that rows with a large mean or a single huge element keep their precision.
+// Both directions are bound by memory: each element is read once and written once.  A group of threads (a warp for rows of
+// up to 512 elements, a CTA beyond) owns fixed columns and walks over rows; gamma, beta and the column sums of the
+// gradients stay in registers all the while, and the next rows are on their way while one is worked on: in registers
+// forward, in a ring of shared memory filled by bulk copies backward.  The variance is summed about the mean, so that
+// rows with a large mean or a single huge element keep their precision: each warp about its own mean, the warps'
+// joined by sum (x - mean)^2 = sum over warps of M_w + n_w (mean_w - mean)^2, which needs one barrier a row.
 // The column sums leave a CTA as one row of partial sums in the workspace; a second kernel adds these rows in
 // a fixed order, which keeps the result independent of scheduling.
 #include <algorithm>
 
+#include "tensor.cuh"
 #include "train.cuh"
 
 namespace slimdp {
 
 namespace {
 
-constexpr uint32_t kLnMaxParts = 592;      // rows of partial column sums; four CTAs on each of 148 SMs
-constexpr uint64_t kLnRegisterDim = 16384; // longest row that stays in registers (1024 threads x 16 elements)
+constexpr uint32_t kLnMaxParts = 1184;     // rows of partial column sums; eight CTAs on each of 148 SMs
+constexpr uint32_t kLnRowsPerPart = 8;     // fewer rows a CTA would make the partial sums a good part of the traffic
 
-// Sum over the THREADS threads of a group, in every thread; `slot` alternates between calls that no barrier separates.
-template <int N, bool WARP, int THREADS>
-__device__ __forceinline__ void group_sum(float (&v)[N], float (&smem)[2][N][32], int slot) {
+// Sum over the THREADS threads of a CTA, in every thread; `slot` alternates between calls that no barrier separates.
+template <int N, int THREADS>
+__device__ __forceinline__ void cta_sum(float (&v)[N], float (&smem)[2][N][32], int slot) {
+    constexpr int kWarps = THREADS / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-    if constexpr (!WARP) {
-        constexpr int kWarps = THREADS / 32;
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        if (lane == 0) {
+    if (lane == 0) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) smem[slot][i][warp] = v[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float s = lane < kWarps ? smem[slot][i][lane] : 0.0f;
-            v[i] = warp_sum(s);
-        }
+        for (int i = 0; i < N; ++i) smem[slot][i][warp] = v[i];
     }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < kWarps ? smem[slot][i][lane] : 0.0f);
 }
 
-template <typename T, int VEC, int ELEMS, int THREADS, bool WARP>
-__global__ void __launch_bounds__(THREADS) ln_forward_kernel(const T* __restrict__ x, uint64_t ldx, uint32_t rows,
-                                                             uint32_t dim, const float* __restrict__ gamma,
-                                                             const float* __restrict__ beta, float eps,
-                                                             T* __restrict__ y, uint64_t ldy, float* __restrict__ mean,
-                                                             float* __restrict__ rstd) {
-    constexpr int kGroup = WARP ? 32 : THREADS, kItems = ELEMS / VEC;
-    __shared__ float smem[2][1][32];
-    const uint32_t t = WARP ? (threadIdx.x & 31) : threadIdx.x;
-    const uint32_t group = WARP ? (threadIdx.x >> 5) : 0, groups = THREADS / kGroup;
+// Sum over groups of WARPS lanes, in every lane.
+template <int WARPS>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int d = WARPS / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    return v;
+}
+
+// Elements of a row of dim that warp w of a group of GROUP threads holds.
+template <int VEC, int PIECES, int GROUP>
+__device__ __forceinline__ float held_by_warp(uint32_t w, uint32_t dim) {
+    uint32_t n = 0;
+    for (uint32_t i = 0; i < PIECES; ++i) {
+        const uint32_t start = (i * GROUP + w * 32) * VEC;
+        n += start < dim ? min(dim - start, 32u * VEC) : 0u;
+    }
+    return (float)n;
+}
+
+// VEC parameters from column c on (`none` where there are none): in 16-byte loads where the vector allows; it may start anywhere.
+template <int VEC>
+__device__ __forceinline__ Vals<VEC> parameters(const float* p, uint32_t c, uint32_t dim, float none) {
+    if constexpr (VEC >= 4) {
+        if (p && c + VEC <= dim && (reinterpret_cast<uintptr_t>(p + c) & 15u) == 0) {
+            float f[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; j += 4) {
+                const float4 q = __ldg(reinterpret_cast<const float4*>(p + c + j));
+                f[j] = q.x, f[j + 1] = q.y, f[j + 2] = q.z, f[j + 3] = q.w;
+            }
+            return Vals<VEC>::make([&](int j) { return f[j]; });
+        }
+    }
+    return Vals<VEC>::make([&](int j) { return p && c + j < dim ? __ldg(p + c + j) : none; });
+}
+
+// A group of GROUP threads a row, PIECES pieces of VEC elements a thread; groups of one warp share CTAs of four.
+template <typename T, int VEC, int PIECES, int GROUP>
+__global__ void __launch_bounds__(GROUP == 32 ? 128 : GROUP, GROUP == 32 ? 4 : GROUP < 512 ? 512 / GROUP : 1)
+    ln_forward_kernel(const T* __restrict__ x, uint64_t ldx, uint32_t rows, uint32_t dim, const float* __restrict__ gamma,
+                      const float* __restrict__ beta, float eps, T* __restrict__ y, uint64_t ldy, float* __restrict__ mean,
+                      float* __restrict__ rstd) {
+    using V = Vals<VEC>;
+    constexpr int kWarps = GROUP / 32;
+    constexpr bool kWarpRows = GROUP == 32, kKeep = GROUP < 1024;      // gamma and beta in registers
+    __shared__ float2 moments[2][32];
+    const uint32_t lane = threadIdx.x & 31, warp = kWarpRows ? 0 : threadIdx.x >> 5, t = kWarpRows ? lane : threadIdx.x;
+    const uint32_t group = kWarpRows ? (threadIdx.x >> 5) : 0, groups = kWarpRows ? 4 : 1;
     const float inv_dim = 1.0f / (float)dim;
-    float ga[ELEMS], be[ELEMS];
+    const float n_own = held_by_warp<VEC, PIECES, GROUP>(warp, dim), inv_own = n_own > 0.0f ? 1.0f / n_own : 0.0f;
+    const float n_lane = held_by_warp<VEC, PIECES, GROUP>(lane % kWarps, dim);
+    auto place = [&](int i) { return (i * GROUP + t) * VEC; };
+    auto weight = [&](const float* p, uint32_t c, float none) { return parameters<VEC>(p, c, dim, none); };
+    V ga[kKeep ? PIECES : 1], be[kKeep ? PIECES : 1];
+    if constexpr (kKeep) {
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
+        for (int i = 0; i < PIECES; ++i) ga[i] = weight(gamma, place(i), 1.0f), be[i] = weight(beta, place(i), 0.0f);
+    }
+    const uint64_t step = (uint64_t)gridDim.x * groups;
+    Pack<T, VEC> ahead[PIECES];
+    auto fetch = [&](uint64_t row) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const uint32_t c = (i * kGroup + t) * VEC + j;
-            ga[i * VEC + j] = (gamma && c < dim) ? __ldg(gamma + c) : 1.0f;
-            be[i * VEC + j] = (beta && c < dim) ? __ldg(beta + c) : 0.0f;
-        }
-    for (uint64_t row = (uint64_t)blockIdx.x * groups + group; row < rows; row += (uint64_t)gridDim.x * groups) {
-        const T* xr = x + row * ldx;
-        float v[ELEMS], s[1] = {0.0f};
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim && row < rows) ahead[i] = load_pack<T, VEC>(x + row * ldx + place(i));
+    };
+    uint64_t row = (uint64_t)blockIdx.x * groups + group;
+    fetch(row);
+    int slot = 0;
+    for (; row < rows; row += step, slot ^= 1) {
+        V v[PIECES], s = V::splat(0.0f);
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const uint32_t c = (i * kGroup + t) * VEC;
-            if (c < dim) {
-                unpack<T, VEC>(load_pack<T, VEC>(xr + c), v + i * VEC);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) s[0] += v[i * VEC + j];
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim) {
+                v[i] = V::of(ahead[i]);
+                s = s + v[i];
             }
-        }
-        group_sum<1, WARP, THREADS>(s, smem, 0);
-        const float mu = s[0] * inv_dim;
-        s[0] = 0.0f;
+        fetch(row + step);
+        float mu = warp_sum(s.sum()) * inv_own;
+        s = V::splat(0.0f);
+        const V less = V::splat(-mu);
 #pragma unroll
-        for (int i = 0; i < kItems; ++i)
-            if ((i * kGroup + t) * VEC < dim) {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    v[i * VEC + j] -= mu;
-                    s[0] = fmaf(v[i * VEC + j], v[i * VEC + j], s[0]);
-                }
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim) {
+                const V d = v[i] + less;
+                s = fma(d, d, s);
             }
-        group_sum<1, WARP, THREADS>(s, smem, 1);
-        const float r = 1.0f / sqrtf(s[0] * inv_dim + eps);
+        float m2 = warp_sum(s.sum());
+        if constexpr (!kWarpRows) {
+            if (lane == 0) moments[slot][warp] = make_float2(mu, m2);
+            __syncthreads();
+            const float2 o = moments[slot][lane % kWarps];
+            mu = lanes_sum<kWarps>(n_lane > 0.0f ? n_lane * o.x : 0.0f) * inv_dim;
+            m2 = lanes_sum<kWarps>(n_lane > 0.0f ? fmaf(n_lane * (o.x - mu), o.x - mu, o.y) : 0.0f);
+        }
+        const float r = 1.0f / sqrtf(m2 * inv_dim + eps);
         if (t == 0) {
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
         }
-        T* yr = y + row * ldy;
+        const V off = V::splat(-mu), by = V::splat(r);
+        T* const yr = y + row * ldy;
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const uint32_t c = (i * kGroup + t) * VEC;
-            if (c < dim) {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    v[i * VEC + j] = fmaf(v[i * VEC + j] * r, ga[i * VEC + j], be[i * VEC + j]);
-                store_pack<T, VEC>(yr + c, v + i * VEC);
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim) {
+                const V g = kKeep ? ga[kKeep ? i : 0] : weight(gamma, place(i), 1.0f);
+                const V b = kKeep ? be[kKeep ? i : 0] : weight(beta, place(i), 0.0f);
+                fma((v[i] + off) * by, g, b).store(yr + place(i));
             }
-        }
     }
 }
 
@@ -119,14 +163,14 @@ __global__ void __launch_bounds__(1024) ln_forward_long_kernel(const T* __restri
         const T* xr = x + row * ldx;
         float s[1] = {0.0f};
         for (uint32_t c = threadIdx.x; c < dim; c += 1024) s[0] += to_f32(xr[c]);
-        group_sum<1, false, 1024>(s, smem, 0);
+        cta_sum<1, 1024>(s, smem, 0);
         const float mu = s[0] / (float)dim;
         s[0] = 0.0f;
         for (uint32_t c = threadIdx.x; c < dim; c += 1024) {
             const float d = to_f32(xr[c]) - mu;
             s[0] = fmaf(d, d, s[0]);
         }
-        group_sum<1, false, 1024>(s, smem, 1);
+        cta_sum<1, 1024>(s, smem, 1);
         const float r = 1.0f / sqrtf(s[0] / (float)dim + eps);
         if (threadIdx.x == 0) {
             if (mean) mean[row] = mu;
@@ -139,102 +183,243 @@ __global__ void __launch_bounds__(1024) ln_forward_long_kernel(const T* __restri
     }
 }
 
+// Two sums over a warp by five exchanges: lanes 0 to 15 end with the first, lanes 16 to 31 with the second.
+__device__ __forceinline__ float warp_sum_two(float a, float b, uint32_t lane) {
+    const bool upper = lane >= 16;
+    float v = upper ? b : a;
+    v += __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    return v;
+}
+
 // parts: [gridDim.x][2][dim] partial column sums of dy h and dy, or NULL.
-template <typename T, int VEC, int ELEMS, int THREADS, bool WARP>
-__global__ void __launch_bounds__(THREADS) ln_backward_kernel(const T* __restrict__ dy, uint64_t lddy,
-                                                              const T* __restrict__ x, uint64_t ldx, uint32_t rows,
-                                                              uint32_t dim, const float* __restrict__ gamma,
-                                                              const float* __restrict__ mean,
-                                                              const float* __restrict__ rstd, T* __restrict__ dx,
-                                                              uint64_t lddx, float* __restrict__ parts) {
-    constexpr int kGroup = WARP ? 32 : THREADS, kItems = ELEMS / VEC;
-    __shared__ float smem[2][2][32];
-    const uint32_t t = WARP ? (threadIdx.x & 31) : threadIdx.x;
-    const uint32_t group = WARP ? (threadIdx.x >> 5) : 0, groups = THREADS / kGroup;
+template <typename T, int VEC, int PIECES, int GROUP>
+__global__ void __launch_bounds__(GROUP == 32 ? 128 : GROUP)
+    ln_backward_kernel(const T* __restrict__ dy, uint64_t lddy, const T* __restrict__ x, uint64_t ldx, uint32_t rows,
+                       uint32_t dim, const float* __restrict__ gamma, const float* __restrict__ mean,
+                       const float* __restrict__ rstd, T* __restrict__ dx, uint64_t lddx, float* __restrict__ parts) {
+    using V = Vals<VEC>;
+    constexpr int kWarps = GROUP / 32;
+    constexpr bool kWarpRows = GROUP == 32;
+    __shared__ float2 sums[2][32];
+    const uint32_t lane = threadIdx.x & 31, warp = kWarpRows ? 0 : threadIdx.x >> 5, t = kWarpRows ? lane : threadIdx.x;
+    const uint32_t group = kWarpRows ? (threadIdx.x >> 5) : 0, groups = kWarpRows ? 4 : 1;
     const float inv_dim = 1.0f / (float)dim;
-    float ga[ELEMS], sum_h[ELEMS], sum_1[ELEMS];
+    auto place = [&](int i) { return (i * GROUP + t) * VEC; };
+    V ga[PIECES], sum_h[PIECES], sum_1[PIECES];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
+    for (int i = 0; i < PIECES; ++i) {
+        ga[i] = parameters<VEC>(gamma, place(i), dim, 1.0f);
+        sum_h[i] = sum_1[i] = V::splat(0.0f);
+    }
+    const uint64_t step = (uint64_t)gridDim.x * groups;
+    Pack<T, VEC> ahead_x[PIECES], ahead_dy[PIECES];
+    float ahead_mu = 0.0f, ahead_r = 0.0f;
+    auto fetch = [&](uint64_t row) {
+        if (row >= rows) return;
+        ahead_mu = __ldg(mean + row), ahead_r = __ldg(rstd + row);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const uint32_t c = (i * kGroup + t) * VEC + j;
-            ga[i * VEC + j] = (gamma && c < dim) ? __ldg(gamma + c) : 1.0f;
-            sum_h[i * VEC + j] = sum_1[i * VEC + j] = 0.0f;
-        }
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim) {
+                ahead_x[i] = load_pack<T, VEC>(x + row * ldx + place(i));
+                ahead_dy[i] = load_pack<T, VEC>(dy + row * lddy + place(i));
+            }
+    };
     int slot = 0;
-    for (uint64_t row = (uint64_t)blockIdx.x * groups + group; row < rows; row += (uint64_t)gridDim.x * groups) {
-        const T *xr = x + row * ldx, *dyr = dy + row * lddy;
-        const float mu = __ldg(mean + row), r = __ldg(rstd + row);
-        float h[ELEMS], g[ELEMS], s[2] = {0.0f, 0.0f};
+    uint64_t row = (uint64_t)blockIdx.x * groups + group;
+    fetch(row);
+    for (; row < rows; row += step, slot ^= 1) {
+        const float mu = ahead_mu, r = ahead_r;
+        V h[PIECES], g[PIECES], s0 = V::splat(0.0f), s1 = s0;
+        const V off = V::splat(-mu), by = V::splat(r);
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const uint32_t c = (i * kGroup + t) * VEC;
-            if (c < dim) {
-                unpack<T, VEC>(load_pack<T, VEC>(xr + c), h + i * VEC);
-                unpack<T, VEC>(load_pack<T, VEC>(dyr + c), g + i * VEC);
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim) h[i] = V::of(ahead_x[i]), g[i] = V::of(ahead_dy[i]);
+        fetch(row + step);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim) {
+                h[i] = (h[i] + off) * by;
+                sum_h[i] = fma(g[i], h[i], sum_h[i]);
+                sum_1[i] = sum_1[i] + g[i];
+                g[i] = g[i] * ga[i];
+                s0 = s0 + g[i];
+                s1 = fma(g[i], h[i], s1);
             }
+        float a = s0.sum(), b = s1.sum();
+        if constexpr (kWarpRows) {
+            a = warp_sum(a), b = warp_sum(b);
+        } else {
+            const float both = warp_sum_two(a, b, lane);
+            if (lane == 0) sums[slot][warp].x = both;
+            if (lane == 16) sums[slot][warp].y = both;
+            __syncthreads();
+            const float2 o = sums[slot][lane % kWarps];
+            a = lanes_sum<kWarps>(o.x), b = lanes_sum<kWarps>(o.y);
         }
+        const V less = V::splat(-a * inv_dim), along = V::splat(-b * inv_dim);
+        T* const dxr = dx + row * lddx;
 #pragma unroll
-        for (int i = 0; i < kItems; ++i)
-            if ((i * kGroup + t) * VEC < dim) {
-#pragma unroll
-                for (int e = i * VEC; e < (i + 1) * VEC; ++e) {
-                    h[e] = (h[e] - mu) * r;
-                    sum_h[e] = fmaf(g[e], h[e], sum_h[e]);
-                    sum_1[e] += g[e];
-                    g[e] *= ga[e];
-                    s[0] += g[e];
-                    s[1] = fmaf(g[e], h[e], s[1]);
-                }
-            }
-        group_sum<2, WARP, THREADS>(s, smem, slot);
-        slot ^= 1;
-        const float a = s[0] * inv_dim, b = s[1] * inv_dim;
-        T* dxr = dx + row * lddx;
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const uint32_t c = (i * kGroup + t) * VEC;
-            if (c < dim) {
-#pragma unroll
-                for (int e = i * VEC; e < (i + 1) * VEC; ++e) g[e] = r * (g[e] - fmaf(h[e], b, a));
-                store_pack<T, VEC>(dxr + c, g + i * VEC);
-            }
-        }
+        for (int i = 0; i < PIECES; ++i)
+            if (place(i) < dim) (by * (g[i] + fma(h[i], along, less))).store(dxr + place(i));
     }
     if (!parts) return;
-    float* part = parts + (uint64_t)blockIdx.x * 2 * dim;
-    if constexpr (WARP) {
+    float* const part = parts + (uint64_t)blockIdx.x * 2 * dim;
+    if constexpr (kWarpRows) {
         // the warps add their column sums one after the other: a fixed order
-        __shared__ float column[2][32 * ELEMS];
+        __shared__ float column[2][32 * VEC * PIECES];
         for (uint32_t w = 0; w < groups; ++w) {
             if (w == group) {
 #pragma unroll
-                for (int i = 0; i < kItems; ++i)
+                for (int i = 0; i < PIECES; ++i)
 #pragma unroll
                     for (int j = 0; j < VEC; ++j) {
-                        const uint32_t c = (i * 32 + t) * VEC + j;
-                        column[0][c] = (w ? column[0][c] : 0.0f) + sum_h[i * VEC + j];
-                        column[1][c] = (w ? column[1][c] : 0.0f) + sum_1[i * VEC + j];
+                        const uint32_t c = place(i) + j;
+                        column[0][c] = (w ? column[0][c] : 0.0f) + sum_h[i].get(j);
+                        column[1][c] = (w ? column[1][c] : 0.0f) + sum_1[i].get(j);
                     }
             }
             __syncthreads();
         }
-        for (uint32_t c = threadIdx.x; c < dim; c += THREADS) {
+        for (uint32_t c = threadIdx.x; c < dim; c += 128) {
             part[c] = column[0][c];
             part[dim + c] = column[1][c];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kItems; ++i)
+        for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const uint32_t c = (i * kGroup + t) * VEC + j;
+            for (int j = 0; j < VEC; ++j)
+                if (place(i) + j < dim) {
+                    part[place(i) + j] = sum_h[i].get(j);
+                    part[dim + place(i) + j] = sum_1[i].get(j);
+                }
+    }
+}
+
+// A wait for a copy ran out on this device (never, unless the device misbehaves).
+__device__ int g_layernorm_status;
+
+constexpr uint32_t kRingMost = 4, kRingLeast = 3;       // rows of the ring
+constexpr uint32_t kRingBytes = 204800;                  // of shared memory an SM gives to rings
+
+// Backward by a CTA a row whose rows start on 16-byte boundaries.  Bulk copies bring x and dy into a ring of `stages` rows of
+// shared memory.  A row is walked twice there: for its two sums (and the column sums), and for dx; the first walk of a
+// row comes before the second of the one before it, so that the reduction between the two is hidden, with one barrier a row.
+template <typename T, int PIECES, int GROUP>
+__global__ void __launch_bounds__(GROUP, GROUP < 512 ? 512 / GROUP : 1)
+    ln_backward_ring_kernel(const T* __restrict__ dy, uint64_t lddy, const T* __restrict__ x, uint64_t ldx, uint32_t rows,
+                            uint32_t dim, const float* __restrict__ gamma, const float* __restrict__ mean,
+                            const float* __restrict__ rstd, T* __restrict__ dx, uint64_t lddx, float* __restrict__ parts,
+                            uint32_t stages) {
+    constexpr int VEC = kVec<T>, kWarps = GROUP / 32;
+    using V = Vals<VEC>;
+    constexpr bool kKeep = GROUP < 1024;                 // 1024 threads leave no registers for gamma
+    extern __shared__ __align__(128) uint8_t ring[];     // [stages][x, dy][dim]
+    __shared__ float2 sums[2][32];
+    __shared__ uint64_t bars[kRingMost];
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bytes = dim * (uint32_t)sizeof(T);
+    const float inv_dim = 1.0f / (float)dim;
+    auto place = [&](int i) { return (i * GROUP + tid) * VEC; };
+    auto weight = [&](uint32_t c) { return parameters<VEC>(gamma, c, dim, 1.0f); };
+    V ga[kKeep ? PIECES : 1], sum_h[PIECES], sum_1[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        if constexpr (kKeep) ga[i] = weight(place(i));
+        sum_h[i] = sum_1[i] = V::splat(0.0f);
+    }
+    if (tid == 0) {
+        for (uint32_t s = 0; s < stages; ++s) mbar_init(smem_addr(bars + s), 1);
+        mbar_init_fence();
+    }
+    __syncthreads();
+    auto request = [&](uint64_t row, uint32_t s) {
+        if (tid != 0 || row >= rows) return;
+        const uint32_t bar = smem_addr(bars + s), dst = smem_addr(ring) + s * 2 * bytes;
+        mbar_expect_tx(bar, 2 * bytes);
+        bulk_load(dst, x + row * ldx, bytes, bar);
+        bulk_load(dst + bytes, dy + row * lddy, bytes, bar);
+    };
+    const uint64_t first = blockIdx.x, step = gridDim.x;
+    for (uint32_t s = 0; s < stages; ++s) request(first + s * step, s);
+    float next_mu = 0.0f, next_r = 0.0f;
+    auto fetch = [&](uint64_t row) {
+        if (row < rows) next_mu = __ldg(mean + row), next_r = __ldg(rstd + row);
+    };
+    fetch(first);
+
+    bool ok = true;
+    uint32_t sa = 0, pa = 0, sb = 0, slot = 0;           // stage and phase of the first walk, stage of the second
+    float mu_b = 0.0f, r_b = 0.0f;
+    for (uint64_t row = first; row < rows + step && ok; row += step) {      // first walk of `row`, second of row - step
+        const float mu_a = next_mu, r_a = next_r;
+        if (row < rows) {
+            fetch(row + step);
+            ok = mbar_wait(smem_addr(bars + sa), pa);
+            const T* const sx = reinterpret_cast<const T*>(ring + sa * 2 * bytes);
+            const T* const sdy = sx + dim;
+            const V off = V::splat(-mu_a), by = V::splat(r_a);
+            V s0 = V::splat(0.0f), s1 = s0;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const uint32_t c = place(i);
                 if (c < dim) {
-                    part[c] = sum_h[i * VEC + j];
-                    part[dim + c] = sum_1[i * VEC + j];
+                    const V h = (V::of(load_pack<T, VEC>(sx + c)) + off) * by;
+                    V g = V::of(load_pack<T, VEC>(sdy + c));
+                    sum_h[i] = fma(g, h, sum_h[i]);
+                    sum_1[i] = sum_1[i] + g;
+                    g = g * (kKeep ? ga[kKeep ? i : 0] : weight(c));
+                    s0 = s0 + g;
+                    s1 = fma(g, h, s1);
                 }
             }
+            const float s = warp_sum_two(s0.sum(), s1.sum(), lane);
+            if (lane == 0) sums[slot][warp].x = s;
+            if (lane == 16) sums[slot][warp].y = s;
+            if (++sa == stages) sa = 0, pa ^= 1u;
+        }
+        if (row != first) {
+            const float2 o = sums[slot ^ 1u][lane % kWarps];
+            const float a = lanes_sum<kWarps>(o.x) * inv_dim, b = lanes_sum<kWarps>(o.y) * inv_dim;
+            const T* const sx = reinterpret_cast<const T*>(ring + sb * 2 * bytes);
+            const T* const sdy = sx + dim;
+            T* const dxr = dx + (row - step) * lddx;
+            // r (g - a - h b), h = (x - mean) r
+            const V off = V::splat(-mu_b), by = V::splat(r_b), less = V::splat(-a * r_b), along = V::splat(-b * r_b * r_b);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const uint32_t c = place(i);
+                if (c < dim) {
+                    const V d = V::of(load_pack<T, VEC>(sx + c)) + off;
+                    const V g = V::of(load_pack<T, VEC>(sdy + c)) * (kKeep ? ga[kKeep ? i : 0] : weight(c));
+                    fma(g, by, fma(d, along, less)).store(dxr + c);
+                }
+            }
+        }
+        ok = !__syncthreads_or(!ok);
+        if (row != first) {
+            request(row - step + stages * step, sb);
+            if (++sb == stages) sb = 0;
+        }
+        mu_b = mu_a, r_b = r_a;
+        slot ^= 1u;
     }
+    if (!ok) {
+        atomicExch(&g_layernorm_status, SLIMDP_ERR_INTERNAL);
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // copies under way end meanwhile
+    }
+    if (!parts) return;
+    float* const part = parts + (uint64_t)blockIdx.x * 2 * dim;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+        if (place(i) < dim)      // dim is a multiple of VEC here, and the workspace 16-byte aligned
+#pragma unroll
+            for (int j = 0; j < VEC; j += 4) {
+                const V &h = sum_h[i], &o = sum_1[i];
+                *reinterpret_cast<float4*>(part + place(i) + j) = make_float4(h.get(j), h.get(j + 1), h.get(j + 2), h.get(j + 3));
+                *reinterpret_cast<float4*>(part + dim + place(i) + j) = make_float4(o.get(j), o.get(j + 1), o.get(j + 2), o.get(j + 3));
+            }
 }
 
 template <typename T>
@@ -255,7 +440,7 @@ __global__ void __launch_bounds__(1024) ln_backward_long_kernel(const T* __restr
             s[0] += g;
             s[1] = fmaf(g, (to_f32(xr[c]) - mu) * r, s[1]);
         }
-        group_sum<2, false, 1024>(s, smem, slot);
+        cta_sum<2, 1024>(s, smem, slot);
         slot ^= 1;
         const float a = s[0] / (float)dim, b = s[1] / (float)dim;
         for (uint32_t c = threadIdx.x; c < dim; c += 1024) {
@@ -285,82 +470,119 @@ __global__ void __launch_bounds__(256) ln_columns_long_kernel(const T* __restric
     part[dim + c] = s1;
 }
 
-// Adds the rows of partial sums: 32 columns a CTA, 8 warps take every eighth row each.
-__global__ void __launch_bounds__(256) ln_reduce_kernel(const float* __restrict__ parts, uint32_t count, uint32_t dim,
-                                                        float* __restrict__ dgamma, float* __restrict__ dbeta,
-                                                        bool accumulate) {
-    __shared__ float smem[8][32];
+// Adds the rows of partial sums: 32 columns a CTA, 32 warps take every 32nd row each.
+__global__ void __launch_bounds__(1024) ln_reduce_kernel(const float* __restrict__ parts, uint32_t count, uint32_t dim,
+                                                         float* __restrict__ dgamma, float* __restrict__ dbeta,
+                                                         bool accumulate) {
+    __shared__ float smem[32][33];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t c = blockIdx.x * 32 + lane;       // of the 2 dim columns of a row of parts
-    const uint32_t width = 2 * dim;
+    const uint64_t width = 2 * (uint64_t)dim, c0 = (uint64_t)blockIdx.x * 32;       // columns of a row of parts
     float s = 0.0f;
-    if (c < width)
-        for (uint32_t p = warp; p < count; p += 8) s += parts[(uint64_t)p * width + c];
+    if (c0 + lane < width) {
+#pragma unroll 4
+        for (uint32_t p = warp; p < count; p += 32) s += parts[p * width + c0 + lane];
+    }
     smem[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < width) {
-        s = smem[0][lane];
-#pragma unroll
-        for (int w = 1; w < 8; ++w) s += smem[w][lane];
-        float* out = c < dim ? dgamma : dbeta;
-        const uint32_t i = c < dim ? c : c - dim;
-        if (out) out[i] = accumulate ? out[i] + s : s;
-    }
+    s = warp_sum(smem[lane][warp]);
+    const uint64_t c = c0 + warp;
+    if (lane != 0 || c >= width) return;
+    float* const out = c < dim ? dgamma : dbeta;
+    const uint64_t i = c < dim ? c : c - dim;
+    if (out) out[i] = accumulate ? out[i] + s : s;
 }
 
-// Calls f.template operator()<ELEMS, THREADS, WARP>() for the shortest group that holds a row of dim elements.
-template <typename F>
-slimdp_status with_shape(uint64_t dim, F&& f) {
-    if (dim <= 256) return f.template operator()<8, 256, true>();
-    if (dim <= 512) return f.template operator()<16, 256, true>();
-    if (dim <= 1024) return f.template operator()<32, 256, true>();
-    if (dim <= 2048) return f.template operator()<8, 256, false>();
-    if (dim <= 4096) return f.template operator()<16, 256, false>();
-    if (dim <= 8192) return f.template operator()<16, 512, false>();
-    return f.template operator()<16, 1024, false>();
+// Calls f.template operator()<PIECES, GROUP>() for the smallest group whose threads hold a row of `pieces` pieces, MOST at most each.
+template <int MOST, typename F>
+slimdp_status with_shape(uint64_t pieces, F&& f) {
+    if (pieces <= 8 * MOST) return f.template operator()<MOST / 4, 32>();
+    if (pieces <= 16 * MOST) return f.template operator()<MOST / 2, 32>();
+    if (pieces <= 32 * MOST) return f.template operator()<MOST, 32>();
+    if (pieces <= 64 * MOST) return f.template operator()<MOST, 64>();
+    if (pieces <= 128 * MOST) return f.template operator()<MOST, 128>();
+    if (pieces <= 256 * MOST) return f.template operator()<MOST, 256>();
+    if (pieces <= 512 * MOST) return f.template operator()<MOST, 512>();
+    return f.template operator()<MOST, 1024>();
 }
 
-template <typename T>
+// Pieces of a thread: four of 16 bytes, or sixteen single elements.
+template <int VEC>
+constexpr int kMostPieces = VEC == 1 ? 16 : 4;
+
+// Longest row that stays in the registers of 1024 threads.
+template <int VEC>
+constexpr uint64_t kLongestRow = 1024ull * kMostPieces<VEC> * VEC;
+
+template <typename T, int VEC>
 struct LnForward {
     const T* x; uint64_t ldx; uint32_t rows, dim; const float *gamma, *beta; float eps; T* y; uint64_t ldy;
-    float *mean, *rstd; bool vec; cudaStream_t st;
+    float *mean, *rstd; cudaStream_t st;
 
-    template <int ELEMS, int THREADS, bool WARP>
+    template <int PIECES, int GROUP>
     slimdp_status operator()() const {
-        const uint32_t groups = WARP ? THREADS / 32 : 1;
-        const uint32_t ctas = (uint32_t)std::min<uint64_t>(((uint64_t)rows + groups - 1) / groups, (uint64_t)sm_count() * (2048 / THREADS));
-        if (vec)
-            ln_forward_kernel<T, kVec<T>, ELEMS, THREADS, WARP><<<ctas, THREADS, 0, st>>>(x, ldx, rows, dim, gamma, beta, eps, y, ldy, mean, rstd);
-        else
-            ln_forward_kernel<T, 1, ELEMS, THREADS, WARP><<<ctas, THREADS, 0, st>>>(x, ldx, rows, dim, gamma, beta, eps, y, ldy, mean, rstd);
+        constexpr int threads = GROUP == 32 ? 128 : GROUP, groups = GROUP == 32 ? 4 : 1;
+        const uint32_t ctas = (uint32_t)std::min<uint64_t>(((uint64_t)rows + groups - 1) / groups, (uint64_t)sm_count() * (threads < 512 ? 512 / threads : 1));    // as many as run at once
+        ln_forward_kernel<T, VEC, PIECES, GROUP><<<ctas, threads, 0, st>>>(x, ldx, rows, dim, gamma, beta, eps, y, ldy, mean, rstd);
         SLIMDP_LAUNCHED(1);
         return SLIMDP_OK;
     }
 };
 
-template <typename T>
+template <typename T, int VEC>
 struct LnBackward {
     const T* dy; uint64_t lddy; const T* x; uint64_t ldx; uint32_t rows, dim; const float *gamma, *mean, *rstd; T* dx;
-    uint64_t lddx; float* parts; bool vec; cudaStream_t st; uint32_t* count;
+    uint64_t lddx; float* parts; cudaStream_t st; uint32_t* count;
 
-    template <int ELEMS, int THREADS, bool WARP>
+    template <int PIECES, int GROUP>
     slimdp_status operator()() const {
-        const uint32_t groups = WARP ? THREADS / 32 : 1;
-        const uint32_t ctas = (uint32_t)std::min<uint64_t>(((uint64_t)rows + groups - 1) / groups, std::min<uint64_t>(kLnMaxParts, (uint64_t)sm_count() * (1024 / THREADS)));
+        constexpr int threads = GROUP == 32 ? 128 : GROUP, groups = GROUP == 32 ? 4 : 1;
+        const uint64_t sms = (uint64_t)sm_count(), units = ((uint64_t)rows + groups - 1) / groups;
+        // rows of the ring that each of `per_sm` CTAs of an SM has
+        const uint32_t row_bytes = 2 * dim * (uint32_t)sizeof(T);
+        constexpr int per_sm = GROUP < 512 ? 512 / GROUP : 1;
+        uint32_t stages = std::min(kRingMost, kRingBytes / per_sm / row_bytes), ring_ctas = per_sm;
+        if (stages < kRingLeast) stages = kRingLeast, ring_ctas = kRingBytes / (kRingLeast * row_bytes);
+        const bool ring = VEC > 1 && GROUP > 32 && ring_ctas > 0;
+        const uint64_t most = ring ? sms * ring_ctas : std::min<uint64_t>(kLnMaxParts, sms * (1024 / threads));
+        const uint32_t ctas = (uint32_t)std::min(units, std::min(most, std::max(sms, units / kLnRowsPerPart)));
         *count = ctas;
-        if (vec)
-            ln_backward_kernel<T, kVec<T>, ELEMS, THREADS, WARP><<<ctas, THREADS, 0, st>>>(dy, lddy, x, ldx, rows, dim, gamma, mean, rstd, dx, lddx, parts);
-        else
-            ln_backward_kernel<T, 1, ELEMS, THREADS, WARP><<<ctas, THREADS, 0, st>>>(dy, lddy, x, ldx, rows, dim, gamma, mean, rstd, dx, lddx, parts);
-        SLIMDP_LAUNCHED(1);
-        return SLIMDP_OK;
+        if constexpr (VEC > 1 && GROUP > 32) {
+            if (ring) {
+                auto kernel = ln_backward_ring_kernel<T, PIECES, GROUP>;
+                static DeviceOnce once;
+                if (once.needed()) {
+                    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes) != cudaSuccess) return SLIMDP_ERR_CUDA;
+                    once.mark();
+                }
+                kernel<<<ctas, GROUP, stages * row_bytes, st>>>(dy, lddy, x, ldx, rows, dim, gamma, mean, rstd, dx, lddx, parts, stages);
+                SLIMDP_LAUNCHED(1);
+                return SLIMDP_OK;
+            }
+        }
+        if constexpr (VEC == 1 || GROUP == 32) {
+            ln_backward_kernel<T, VEC, PIECES, GROUP><<<ctas, threads, 0, st>>>(dy, lddy, x, ldx, rows, dim, gamma, mean, rstd, dx, lddx, parts);
+            SLIMDP_LAUNCHED(1);
+            return SLIMDP_OK;
+        }
+        return SLIMDP_ERR_UNSUPPORTED;       // not reached: see backward_on_chip
     }
 };
+
+// Whether rows stay on chip between their sums and their result; longer ones are read once more.
+bool backward_on_chip(uint64_t dim, int32_t type, bool vec) {
+    if (!vec) return dim <= 8192;            // 1024 threads would spill
+    return dim * type_bytes(type) <= 65536 && kRingLeast * 2 * dim * type_bytes(type) <= kRingBytes;
+}
 
 }  // namespace
 
 size_t layernorm_ws_bytes(uint64_t rows, uint64_t dim) {
     return align_up(std::max<uint64_t>(1, std::min<uint64_t>(rows, kLnMaxParts)) * 2 * dim * sizeof(float), 16);
+}
+
+slimdp_status read_layernorm_status() {
+    int status = 0;
+    return cudaMemcpyFromSymbol(&status, g_layernorm_status, sizeof(status)) == cudaSuccess ? status : SLIMDP_ERR_CUDA;
 }
 
 slimdp_status launch_layernorm_forward(const void* x, uint64_t ldx, uint32_t rows, uint32_t dim, int32_t type,
@@ -369,13 +591,15 @@ slimdp_status launch_layernorm_forward(const void* x, uint64_t ldx, uint32_t row
     const bool vec = rows_vectorise(x, ldx, dim, type) && rows_vectorise(y, ldy, dim, type);
     return with_type(type, [&](auto e) -> slimdp_status {
         using T = decltype(e);
-        if (dim > kLnRegisterDim) {
-            const uint32_t ctas = (uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 2);
-            ln_forward_long_kernel<T><<<ctas, 1024, 0, st>>>((const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd);
-            SLIMDP_LAUNCHED(1);
-            return SLIMDP_OK;
-        }
-        return with_shape(dim, LnForward<T>{(const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd, vec, st});
+        constexpr int V = kVec<T>;
+        if (vec && dim <= kLongestRow<V>)
+            return with_shape<kMostPieces<V>>((dim + V - 1) / V, LnForward<T, V>{(const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd, st});
+        if (dim <= kLongestRow<1>)
+            return with_shape<kMostPieces<1>>(dim, LnForward<T, 1>{(const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd, st});
+        const uint32_t ctas = (uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 2);
+        ln_forward_long_kernel<T><<<ctas, 1024, 0, st>>>((const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd);
+        SLIMDP_LAUNCHED(1);
+        return SLIMDP_OK;
     });
 }
 
@@ -389,7 +613,8 @@ slimdp_status launch_layernorm_backward(const void* dy, uint64_t lddy, const voi
     if (rows > 0) {
         const slimdp_status s = with_type(type, [&](auto e) -> slimdp_status {
             using T = decltype(e);
-            if (dim > kLnRegisterDim) {
+            constexpr int V = kVec<T>;
+            if (!backward_on_chip(dim, type, vec)) {
                 const uint32_t ctas = (uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 2);
                 ln_backward_long_kernel<T><<<ctas, 1024, 0, st>>>((const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx);
                 SLIMDP_LAUNCHED(1);
@@ -400,12 +625,14 @@ slimdp_status launch_layernorm_backward(const void* dy, uint64_t lddy, const voi
                 }
                 return SLIMDP_OK;
             }
-            return with_shape(dim, LnBackward<T>{(const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, vec, st, &count});
+            if (vec)
+                return with_shape<kMostPieces<V>>((dim + V - 1) / V, LnBackward<T, V>{(const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, st, &count});
+            return with_shape<kMostPieces<1>>(dim, LnBackward<T, 1>{(const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, st, &count});
         });
         if (s != SLIMDP_OK) return s;
     }
     if (parts) {
-        ln_reduce_kernel<<<(unsigned)((2 * (uint64_t)dim + 31) / 32), 256, 0, st>>>(parts, count, dim, dgamma, dbeta, accumulate);
+        ln_reduce_kernel<<<(unsigned)((2 * (uint64_t)dim + 31) / 32), 1024, 0, st>>>(parts, count, dim, dgamma, dbeta, accumulate);
         SLIMDP_LAUNCHED(1);
     }
     return SLIMDP_OK;

@@ -422,10 +422,11 @@ __global__ void __launch_bounds__(256) join_kernel(const ProductArgs args) {
     }
 }
 
-// db (+)= sum over rows of dy.  A cluster of eight CTAs takes 32 V columns, each of its 128 warps every 128th row; sums go from
-// registers to shared memory to rank 0, in a fixed order.  Bound by reading dy: sixteen warps with four 16-byte loads a
+// db (+)= sum over rows of dy.  A cluster of eight CTAs takes 32 V columns, each of its 256 warps every 256th row; sums go from
+// registers to shared memory to rank 0, in a fixed order.  Bound by reading dy: 32 warps with eight 16-byte loads a
 // thread in flight keep an SM's share of the bandwidth busy.
-constexpr uint32_t kSumRanks = 8, kSumWarps = 16;
+constexpr uint32_t kSumRanks = 8, kSumWarps = 32;
+constexpr int kSumAhead = 8;
 
 template <typename T, int V>
 __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWarps)
@@ -438,12 +439,12 @@ __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWar
     float s[V] = {};
     if (j + V <= n) {
         uint64_t i = rank * kSumWarps + warp;
-        for (; i + 3 * stride < m; i += 4 * stride) {
-            Pack<T, V> p[4];
+        for (; i + (kSumAhead - 1) * stride < m; i += kSumAhead * stride) {
+            Pack<T, V> p[kSumAhead];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) p[u] = load_pack<T, V>(dy + (i + u * stride) * lddy + j);
+            for (int u = 0; u < kSumAhead; ++u) p[u] = load_pack<T, V>(dy + (i + u * stride) * lddy + j);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < kSumAhead; ++u) {
                 float f[V];
                 unpack<T, V>(p[u], f);
 #pragma unroll
@@ -527,17 +528,16 @@ __global__ void __launch_bounds__(256) pack_kernel(PackJob job0, PackJob job1) {
     for (uint64_t g = (uint64_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (uint64_t)gridDim.x * 256) {
         const uint64_t i = g / groups, j = (g - i * groups) * 8;
         const T* const src = (const T*)job.src + i * job.ld + j;
-        T v[8];
-        if (job.wide && j + 8 <= job.cols) {
-#pragma unroll
-            for (int u = 0; u < 8; u += kVec<T>) *reinterpret_cast<Pack<T, kVec<T>>*>(v + u) = load_pack<T, kVec<T>>(src + u);
-        } else {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = j + u < job.cols ? src[u] : T(0.0f);
-        }
         // ld_dst is a multiple of eight: whole groups fit
         if constexpr (sizeof(T) == 4) {
-            float part[8][3];
+            float v[8], part[8][3];
+            if (job.wide && j + 8 <= job.cols) {
+                unpack<T, 4>(load_pack<T, 4>(src), v);
+                unpack<T, 4>(load_pack<T, 4>(src + 4), v + 4);
+            } else {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] = j + u < job.cols ? src[u] : 0.0f;
+            }
 #pragma unroll
             for (int u = 0; u < 8; ++u) cut(v[u], part[u]);
 #pragma unroll
@@ -548,7 +548,15 @@ __global__ void __launch_bounds__(256) pack_kernel(PackJob job0, PackJob job1) {
                 store_pack<__nv_bfloat16, 8>((__nv_bfloat16*)job.dst + ((uint64_t)p * job.rows + i) * job.ld_dst + j, f);
             }
         } else {
-            *reinterpret_cast<Pack<T, 8>*>((T*)job.dst + i * job.ld_dst + j) = *reinterpret_cast<Pack<T, 8>*>(v);
+            // 16-bit operands come here only where their rows are not on 16-byte boundaries; values move as they are
+            const uint16_t* const bits = (const uint16_t*)src;
+            uint32_t w[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t lo = j + 2 * u < job.cols ? bits[2 * u] : 0u, hi = j + 2 * u + 1 < job.cols ? bits[2 * u + 1] : 0u;
+                w[u] = lo | hi << 16;
+            }
+            *reinterpret_cast<uint4*>((T*)job.dst + i * job.ld_dst + j) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
 }

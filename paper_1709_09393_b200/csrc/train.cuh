@@ -37,21 +37,50 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
-// N adjacent elements as one access; N sizeof(T) is 16 for a vector access and sizeof(T) for a scalar one.
+// N adjacent elements as one access; N sizeof(T) is 16 for a vector access and sizeof(T) for a scalar one.  Vectors of
+// 16-bit types are four words: an array of them would not stay in registers.
 template <typename T, int N>
 struct alignas(N * sizeof(T)) Pack {
     T v[N];
+    __device__ __forceinline__ float get(int i) const { return to_f32(v[i]); }
+};
+template <>
+struct alignas(16) Pack<__nv_bfloat16, 8> {
+    uint32_t w[4];
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); }
+};
+template <>
+struct alignas(16) Pack<__half, 8> {
+    uint32_t w[4];
+    __device__ __forceinline__ float get(int i) const {
+        const __half2 h = *reinterpret_cast<const __half2*>(&w[i / 2]);
+        return i % 2 ? __high2float(h) : __low2float(h);
+    }
 };
 
 template <typename T, int N>
 __device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
-    return *reinterpret_cast<const Pack<T, N>*>(p);
+    if constexpr (N * sizeof(T) == 16) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p);
+        Pack<T, N> r;
+        if constexpr (sizeof(T) == 2) {
+            r.w[0] = q.x, r.w[1] = q.y, r.w[2] = q.z, r.w[3] = q.w;
+        } else {
+            r.v[0] = __uint_as_float(q.x), r.v[1] = __uint_as_float(q.y), r.v[2] = __uint_as_float(q.z), r.v[3] = __uint_as_float(q.w);
+        }
+        return r;
+    } else {
+        Pack<T, N> r;
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.v[i] = p[i];
+        return r;
+    }
 }
 
 template <typename T, int N>
 __device__ __forceinline__ void unpack(const Pack<T, N>& p, float* f) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = to_f32(p.v[i]);
+    for (int i = 0; i < N; ++i) f[i] = p.get(i);
 }
 
 // Two values rounded and packed by one instruction.
@@ -71,16 +100,125 @@ __device__ __forceinline__ void store_pack(T* p, const float* f) {
     if constexpr (sizeof(T) == 2 && N == 8) {
         *reinterpret_cast<uint4*>(p) = make_uint4(pack_two<T>(f[0], f[1]), pack_two<T>(f[2], f[3]), pack_two<T>(f[4], f[5]), pack_two<T>(f[6], f[7]));
     } else {
-        Pack<T, N> r;
+        if constexpr (sizeof(T) == 4 && N == 4) {
+            *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) r.v[i] = from_f32<T>(f[i]);
-        *reinterpret_cast<Pack<T, N>*>(p) = r;
+            for (int i = 0; i < N; ++i) p[i] = from_f32<T>(f[i]);
+        }
     }
 }
 
 // Elements of a 16-byte access.
 template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);
+
+// Two fp32 values in one register pair; the packed instructions do both at the price of one.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split_pair(uint64_t p, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// N adjacent values of fp32, worked on in pairs; one value alone where N is 1.
+template <int N>
+struct Vals {
+    uint64_t p[N / 2];
+
+    static __device__ __forceinline__ Vals splat(float f) {
+        Vals r;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) r.p[i] = pair_of(f, f);
+        return r;
+    }
+    template <typename F>
+    static __device__ __forceinline__ Vals make(F&& f) {
+        Vals r;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) r.p[i] = pair_of(f(2 * i), f(2 * i + 1));
+        return r;
+    }
+    template <typename T>
+    static __device__ __forceinline__ Vals of(const Pack<T, N>& k) {
+        return make([&](int i) { return k.get(i); });
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* to) const {
+        float f[N];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) split_pair(p[i], f[2 * i], f[2 * i + 1]);
+        store_pack<T, N>(to, f);
+    }
+    __device__ __forceinline__ float get(int i) const {
+        float lo, hi;
+        split_pair(p[i / 2], lo, hi);
+        return i % 2 ? hi : lo;
+    }
+    __device__ __forceinline__ float sum() const {
+        uint64_t s = p[0];
+#pragma unroll
+        for (int i = 1; i < N / 2; ++i) s = add_pair(s, p[i]);
+        float lo, hi;
+        split_pair(s, lo, hi);
+        return lo + hi;
+    }
+};
+template <>
+struct Vals<1> {
+    float p[1];
+
+    static __device__ __forceinline__ Vals splat(float f) { return {{f}}; }
+    template <typename F>
+    static __device__ __forceinline__ Vals make(F&& f) { return {{f(0)}}; }
+    template <typename T>
+    static __device__ __forceinline__ Vals of(const Pack<T, 1>& k) { return {{k.get(0)}}; }
+    template <typename T>
+    __device__ __forceinline__ void store(T* to) const { *to = from_f32<T>(p[0]); }
+    __device__ __forceinline__ float get(int) const { return p[0]; }
+    __device__ __forceinline__ float sum() const { return p[0]; }
+};
+__device__ __forceinline__ float fma_pair(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float add_pair(float a, float b) { return a + b; }
+__device__ __forceinline__ float mul_pair(float a, float b) { return a * b; }
+template <int N>
+__device__ __forceinline__ Vals<N> fma(const Vals<N>& a, const Vals<N>& b, const Vals<N>& c) {
+    Vals<N> r;
+#pragma unroll
+    for (int i = 0; i < (N + 1) / 2; ++i) r.p[i] = fma_pair(a.p[i], b.p[i], c.p[i]);
+    return r;
+}
+template <int N>
+__device__ __forceinline__ Vals<N> operator+(const Vals<N>& a, const Vals<N>& b) {
+    Vals<N> r;
+#pragma unroll
+    for (int i = 0; i < (N + 1) / 2; ++i) r.p[i] = add_pair(a.p[i], b.p[i]);
+    return r;
+}
+template <int N>
+__device__ __forceinline__ Vals<N> operator*(const Vals<N>& a, const Vals<N>& b) {
+    Vals<N> r;
+#pragma unroll
+    for (int i = 0; i < (N + 1) / 2; ++i) r.p[i] = mul_pair(a.p[i], b.p[i]);
+    return r;
+}
 
 // Whether every row of a matrix can be read in 16-byte pieces from its start to its end.
 inline bool rows_vectorise(const void* p, uint64_t ld, uint64_t cols, int32_t type) {

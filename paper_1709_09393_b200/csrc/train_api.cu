@@ -31,6 +31,7 @@ slimdp_status launch_activation_backward(const void* dy, uint64_t lddy, const vo
                                          cudaStream_t st);
 slimdp_status read_product_status();
 slimdp_status read_distill_status();
+slimdp_status read_layernorm_status();
 slimdp_status launch_distill(const void* logits, uint64_t ldl, uint32_t rows, uint32_t vocab, int32_t type,
                              const int32_t* idx, const void* teacher, int32_t teacher_type, uint32_t top,
                              const int32_t* label, const float* weight, float temperature, float kd, float ce,
@@ -164,8 +165,9 @@ slimdp_status slimdp_activation_backward(const void* dy, uint64_t lddy, const vo
 
 slimdp_status slimdp_train_read_status(void* stream) {
     if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return SLIMDP_ERR_CUDA;
-    const slimdp_status s = read_product_status();
-    return s != SLIMDP_OK ? s : read_distill_status();
+    slimdp_status s = read_product_status();
+    if (s == SLIMDP_OK) s = read_distill_status();
+    return s == SLIMDP_OK ? read_layernorm_status() : s;
 }
 
 slimdp_status slimdp_distill(const void* logits, uint64_t ldl, uint64_t rows, uint64_t vocab, int32_t type,

@@ -16,26 +16,35 @@ from . import binding as B
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
-_lib, _check, _stream = B.lib, B._check, B._stream
+_lib, _check = B.lib, B._check
+_F32 = torch.float32
+_current_stream = torch._C._cuda_getCurrentRawStream     # torch.cuda.current_stream() makes an object for 3 us a call
 
 
-def _type(t: torch.Tensor, name: str) -> int:
+def _stream(stream, t: torch.Tensor) -> int:
+    return _current_stream(t.get_device()) if stream is None else stream.cuda_stream
+
+
+def _leading(t: torch.Tensor, name: str):
+    """The matrix that sets a call's type: (type code, dtype, shape)."""
     code = _TYPES.get(t.dtype)
-    if code is None or not t.is_cuda or t.dim() != 2:
+    shape = t.shape
+    if code is None or not t.is_cuda or len(shape) != 2:
         raise TypeError(f"{name}: expected a 2-D CUDA tensor of float32, bfloat16 or float16")
-    return code
+    return code, t.dtype, shape
 
 
-def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, name: str):
+def _matrix(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str):
     """(address, row stride) of a matrix; (NULL, cols) for a missing one."""
+    rows, cols = shape
     if t is None:
         return None, cols
-    if t.dtype != dtype or not t.is_cuda or t.dim() != 2:
+    if t.dtype is not dtype or not t.is_cuda:
         raise TypeError(f"{name}: expected a 2-D CUDA tensor of {dtype}")
-    if t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name}: expected {rows} x {cols}, got {t.shape[0]} x {t.shape[1]}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected {rows} x {cols}, got {tuple(t.shape)}")
     ld, step = t.stride()
-    if cols > 1 and step != 1:
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: columns are not adjacent")
     if rows <= 1:
         ld = cols
@@ -44,10 +53,10 @@ def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype,
     return t.data_ptr() or None, ld
 
 
-def _vector(t: Optional[torch.Tensor], n: int, name: str, dtype: torch.dtype = torch.float32) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], n: int, name: str, dtype: torch.dtype = _F32) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
     if t.numel() != n:
         raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
@@ -82,101 +91,101 @@ def linear_workspace_bytes(m: int, n: int, k: int, dtype: torch.dtype) -> int:
 def slimdp_layernorm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                              y: torch.Tensor, mean: Optional[torch.Tensor] = None,
                              rstd: Optional[torch.Tensor] = None, stream=None):
-    code = _type(x, "x")
-    rows, dim = x.shape
-    px, ldx = _matrix(x, rows, dim, x.dtype, "x")
-    py, ldy = _matrix(y, rows, dim, x.dtype, "y")
+    code, dtype, shape = _leading(x, "x")
+    rows, dim = shape
+    px, ldx = _matrix(x, shape, dtype, "x")
+    py, ldy = _matrix(y, shape, dtype, "y")
     _check("slimdp_layernorm_forward",
            _lib.slimdp_layernorm_forward(px, ldx, rows, dim, code, _vector(gamma, dim, "gamma"),
                                          _vector(beta, dim, "beta"), eps, py, ldy, _vector(mean, rows, "mean"),
-                                         _vector(rstd, rows, "rstd"), _stream(stream)))
+                                         _vector(rstd, rows, "rstd"), _stream(stream, x)))
 
 
 def slimdp_layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor,
                               rstd: torch.Tensor, dx: torch.Tensor, dgamma: Optional[torch.Tensor],
                               dbeta: Optional[torch.Tensor], ws: Optional[torch.Tensor], accumulate: bool = False,
                               stream=None):
-    code = _type(x, "x")
-    rows, dim = x.shape
-    pdy, lddy = _matrix(dy, rows, dim, x.dtype, "dy")
-    px, ldx = _matrix(x, rows, dim, x.dtype, "x")
-    pdx, lddx = _matrix(dx, rows, dim, x.dtype, "dx")
+    code, dtype, shape = _leading(x, "x")
+    rows, dim = shape
+    pdy, lddy = _matrix(dy, shape, dtype, "dy")
+    px, ldx = _matrix(x, shape, dtype, "x")
+    pdx, lddx = _matrix(dx, shape, dtype, "dx")
     pws, nws = _ws(ws)
     _check("slimdp_layernorm_backward",
            _lib.slimdp_layernorm_backward(pdy, lddy, px, ldx, rows, dim, code, _vector(gamma, dim, "gamma"),
                                           _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), pdx, lddx,
                                           _vector(dgamma, dim, "dgamma"), _vector(dbeta, dim, "dbeta"),
-                                          bool(accumulate), pws, nws, _stream(stream)))
+                                          bool(accumulate), pws, nws, _stream(stream, x)))
 
 
 def slimdp_linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor,
                           ws: torch.Tensor, activation: str = "none", residual: Optional[torch.Tensor] = None,
                           z: Optional[torch.Tensor] = None, stream=None):
     """y = act(x w^T + bias) + residual; z, if given, receives x w^T + bias."""
-    code, act = _type(x, "x"), _act(activation)
-    _type(w, "w")
-    m, k = x.shape
-    n = w.shape[0]
-    px, ldx = _matrix(x, m, k, x.dtype, "x")
-    pw, ldw = _matrix(w, n, k, x.dtype, "w")
-    pr, ldr = _matrix(residual, m, n, x.dtype, "residual")
-    py, ldy = _matrix(y, m, n, x.dtype, "y")
-    pz, ldz = _matrix(z, m, n, x.dtype, "z")
+    code, dtype, shape = _leading(x, "x")
+    act = _act(activation)
+    m, k = shape
+    n = _leading(w, "w")[2][0]
+    px, ldx = _matrix(x, shape, dtype, "x")
+    pw, ldw = _matrix(w, (n, k), dtype, "w")
+    pr, ldr = _matrix(residual, (m, n), dtype, "residual")
+    py, ldy = _matrix(y, (m, n), dtype, "y")
+    pz, ldz = _matrix(z, (m, n), dtype, "z")
     pws, nws = _ws(ws)
     _check("slimdp_linear_forward",
            _lib.slimdp_linear_forward(px, ldx, pw, ldw, _vector(bias, n, "bias"), pr, ldr, m, n, k, code, act, py, ldy,
-                                      pz, ldz, pws, nws, _stream(stream)))
+                                      pz, ldz, pws, nws, _stream(stream, x)))
 
 
 def slimdp_linear_backward_input(dy: torch.Tensor, w: torch.Tensor, dx: torch.Tensor, ws: torch.Tensor,
                                  activation: str = "none", z: Optional[torch.Tensor] = None,
                                  add: Optional[torch.Tensor] = None, stream=None):
     """dx = (dy w) * act'(z) + add, with z the pre-activation of the layer that made this one's input."""
-    code, act = _type(dy, "dy"), _act(activation)
-    _type(w, "w")
-    m, n = dy.shape
-    k = w.shape[1]
-    pdy, lddy = _matrix(dy, m, n, dy.dtype, "dy")
-    pw, ldw = _matrix(w, n, k, dy.dtype, "w")
-    pz, ldz = _matrix(z, m, k, dy.dtype, "z")
-    pa, lda = _matrix(add, m, k, dy.dtype, "add")
-    pdx, lddx = _matrix(dx, m, k, dy.dtype, "dx")
+    code, dtype, shape = _leading(dy, "dy")
+    act = _act(activation)
+    m, n = shape
+    k = _leading(w, "w")[2][1]
+    pdy, lddy = _matrix(dy, shape, dtype, "dy")
+    pw, ldw = _matrix(w, (n, k), dtype, "w")
+    pz, ldz = _matrix(z, (m, k), dtype, "z")
+    pa, lda = _matrix(add, (m, k), dtype, "add")
+    pdx, lddx = _matrix(dx, (m, k), dtype, "dx")
     pws, nws = _ws(ws)
     _check("slimdp_linear_backward_input",
            _lib.slimdp_linear_backward_input(pdy, lddy, pw, ldw, pz, ldz, pa, lda, m, n, k, code, act, pdx, lddx, pws,
-                                             nws, _stream(stream)))
+                                             nws, _stream(stream, dy)))
 
 
 def slimdp_linear_backward_weight(dy: torch.Tensor, x: torch.Tensor, dw: torch.Tensor, db: Optional[torch.Tensor],
                                   ws: torch.Tensor, accumulate: bool = False, stream=None):
     """dw (+)= dy^T x in float32, db (+)= column sums of dy."""
-    code = _type(dy, "dy")
-    _type(x, "x")
-    m, n = dy.shape
-    k = x.shape[1]
-    pdy, lddy = _matrix(dy, m, n, dy.dtype, "dy")
-    px, ldx = _matrix(x, m, k, dy.dtype, "x")
-    pdw, lddw = _matrix(dw, n, k, torch.float32, "dw")
+    code, dtype, shape = _leading(dy, "dy")
+    m, n = shape
+    k = _leading(x, "x")[2][1]
+    pdy, lddy = _matrix(dy, shape, dtype, "dy")
+    px, ldx = _matrix(x, (m, k), dtype, "x")
+    pdw, lddw = _matrix(dw, (n, k), _F32, "dw")
     pws, nws = _ws(ws)
     _check("slimdp_linear_backward_weight",
            _lib.slimdp_linear_backward_weight(pdy, lddy, px, ldx, m, n, k, code, pdw, lddw, _vector(db, n, "db"),
-                                              bool(accumulate), pws, nws, _stream(stream)))
+                                              bool(accumulate), pws, nws, _stream(stream, dy)))
 
 
 def train_read_status(stream=None) -> None:
     """Synchronises, and raises if a bounded wait of one of these kernels ever ran out on this device."""
-    _check("slimdp_train_read_status", _lib.slimdp_train_read_status(_stream(stream)))
+    _check("slimdp_train_read_status", _lib.slimdp_train_read_status(B._stream(stream)))
 
 
 def slimdp_activation_backward(dy: torch.Tensor, z: torch.Tensor, dz: torch.Tensor, activation: str, stream=None):
     """dz = dy * act'(z)."""
-    code, act = _type(dy, "dy"), _act(activation)
-    m, n = dy.shape
-    pdy, lddy = _matrix(dy, m, n, dy.dtype, "dy")
-    pz, ldz = _matrix(z, m, n, dy.dtype, "z")
-    pdz, lddz = _matrix(dz, m, n, dy.dtype, "dz")
+    code, dtype, shape = _leading(dy, "dy")
+    act = _act(activation)
+    m, n = shape
+    pdy, lddy = _matrix(dy, shape, dtype, "dy")
+    pz, ldz = _matrix(z, shape, dtype, "z")
+    pdz, lddz = _matrix(dz, shape, dtype, "dz")
     _check("slimdp_activation_backward",
-           _lib.slimdp_activation_backward(pdy, lddy, pz, ldz, m, n, code, act, pdz, lddz, _stream(stream)))
+           _lib.slimdp_activation_backward(pdy, lddy, pz, ldz, m, n, code, act, pdz, lddz, _stream(stream, dy)))
 
 
 def slimdp_distill(logits: torch.Tensor, teacher_idx: Optional[torch.Tensor], teacher_logit: Optional[torch.Tensor],
@@ -184,10 +193,10 @@ def slimdp_distill(logits: torch.Tensor, teacher_idx: Optional[torch.Tensor], te
                    row_weight: Optional[torch.Tensor] = None, temperature: float = 1.0, kd_weight: float = 1.0,
                    ce_weight: float = 0.0, stream=None):
     """Loss of each row and its gradient; dlogits may be logits (replaced) or None (the loss alone)."""
-    code = _type(logits, "logits")
-    rows, vocab = logits.shape
-    pl, ldl = _matrix(logits, rows, vocab, logits.dtype, "logits")
-    pd, ldd = _matrix(dlogits, rows, vocab, logits.dtype, "dlogits")
+    code, dtype, shape = _leading(logits, "logits")
+    rows, vocab = shape
+    pl, ldl = _matrix(logits, shape, dtype, "logits")
+    pd, ldd = _matrix(dlogits, shape, dtype, "dlogits")
     if (teacher_idx is None) != (teacher_logit is None):
         raise ValueError("teacher_idx and teacher_logit come together")
     top, pi, pt, tcode = 0, None, None, 0
@@ -206,4 +215,4 @@ def slimdp_distill(logits: torch.Tensor, teacher_idx: Optional[torch.Tensor], te
            _lib.slimdp_distill(pl, ldl, rows, vocab, code, pi, pt, tcode, top,
                                _vector(label, rows, "label", torch.int32), _vector(row_weight, rows, "row_weight"),
                                temperature, kd_weight, ce_weight, _vector(loss, rows, "loss"), pd, ldd,
-                               _stream(stream)))
+                               _stream(stream, logits)))

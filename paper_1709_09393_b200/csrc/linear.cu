@@ -92,7 +92,11 @@ constexpr int kWide = P == kWeight ? 4 : kVec<T>;
 constexpr int kBk = 64;                      // summed indices of a stage: 128 bytes of a 16-bit type
 constexpr uint32_t kChunk = 8;               // blocks of kBk summed indices that stay in one accumulator where T or P asks for fp32 results
 constexpr int kEpilogueWarps = 8;
-constexpr int kProductThreads = 32 * (2 + kEpilogueWarps);
+constexpr int kFirstEpilogueWarp = 4;         // registers are dealt out to groups of four warps
+constexpr int kProductThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
+// Registers of a chunked product's warps: its sums take 128 of an epilogue warp.  The kernel starts with 168 for each of its twelve
+// warps, and 4 x 56 + 8 x 224 = 12 x 168.
+constexpr int kLoaderRegs = 56, kEpilogueRegs = 224;
 constexpr int kEpiloguePitch = 33;           // floats of a row of a warp's 32 x 32 staging square
 
 // A wait in a product kernel ran out on this device (never, unless the device misbehaves).
@@ -204,7 +208,7 @@ __device__ __forceinline__ void tile_place(uint32_t t, uint32_t tiles_m, uint32_
     tn = in / height;
 }
 
-// One 128 CG x BN tile at a time: warp 0 loads, warp 1 of the (leading) CTA multiplies, warps 2 to 9 finish.
+// One 128 CG x BN tile at a time: warp 0 loads, warp 1 of the (leading) CTA multiplies, warps 4 to 11 finish.
 template <typename T, Product P, int CG, int BN>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                      const __grid_constant__ CUtensorMap map_b,
@@ -248,9 +252,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem + (slot - base));
 
+    // Sums of a chunked product take 128 registers of an epilogue warp: the first four warps give up theirs.  384 threads start
+    // with 168 each; 4 x 56 + 8 x 224 = 12 x 168 of a lane.
     bool ok = true;
-    if (warp == 0) {
-        if (lane == 0) {
+    if (warp < kFirstEpilogueWarp) {
+        if constexpr (kChunked<T, P>) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoaderRegs));
+        if (warp == 0 && lane == 0) {
             uint32_t s = 0, phase = 0;
             for (uint32_t item = group; item < items && ok; item += groups) {
                 uint32_t tm, tn;
@@ -285,9 +292,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             if (++s == S::stages) s = 0, phase ^= 1u;
                         }
             }
-        }
-    } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        } else if (warp == 1 && lane == 0 && rank == 0) {
             const uint32_t idesc = (1u << 4) | (args.format << 7) | (args.format << 10) | ((kMnA ? 1u : 0u) << 15) |
                                    ((kMnB ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 * CG >> 4) << 24);
             constexpr uint32_t step_a = (kMnA ? 2048u : 32u) >> 4, step_b = (kMnB ? 2048u : 32u) >> 4;
@@ -317,8 +322,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             }
         }
     } else {
-        const uint32_t quarter = warp & 3u, half = (warp - 2) >> 2;
-        float* const square = reinterpret_cast<float*>(smem + S::stages * S::stage) + (warp - 2) * 32 * kEpiloguePitch;
+        if constexpr (kChunked<T, P>) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
+        const uint32_t quarter = warp & 3u, half = (warp - kFirstEpilogueWarp) >> 2;
+        float* const square = reinterpret_cast<float*>(smem + S::stages * S::stage) + (warp - kFirstEpilogueWarp) * 32 * kEpiloguePitch;
         constexpr int kSquares = BN / 64;             // of 32 x 32 results of this warp
         const uint32_t lanes = tmem + ((quarter * 32) << 16) + half * (BN / 2);
         uint32_t count = 0;
@@ -339,12 +345,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     if (!(ok = mbar_wait(acc_full(count & 1u), (count >> 1) & 1u))) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int q = 0; q < kSquares; ++q) {
-                        float v[32];
-                        tmem_load32(lanes + (count & 1u) * BN + q * 32, v);
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) sum[q][c] += v[c];
-                    }
+                    for (int q = 0; q < 2 * kSquares; ++q)      // 16 columns at a time: 32 more registers would spill
+                        tmem_add16(lanes + (count & 1u) * BN + q * 16, &sum[q / 2][q % 2 * 16]);
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(cluster_addr(acc_empty(count & 1u), 0));
@@ -638,6 +640,11 @@ slimdp_status launch_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, c
     auto kernel = product_kernel<T, P, CG, BN>;
     if (once.needed()) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem) != cudaSuccess) return SLIMDP_ERR_CUDA;
+        // a kernel that started with fewer registers than it deals out to its warps would wait for them for good
+        cudaFuncAttributes attr;
+        if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess) return SLIMDP_ERR_CUDA;
+        if (kChunked<T, P> && attr.numRegs * (kProductThreads / 32) < kFirstEpilogueWarp * kLoaderRegs + kEpilogueWarps * kEpilogueRegs)
+            return SLIMDP_ERR_UNSUPPORTED;
         once.mark();
     }
     cudaLaunchConfig_t cfg = {};

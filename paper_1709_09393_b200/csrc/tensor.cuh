@@ -193,6 +193,20 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// 16 adjacent columns, added to v.
+__device__ __forceinline__ void tmem_add16(uint32_t addr, float* v) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] += __uint_as_float(r[i]);
+}
+
 // Descriptor of an operand tile in shared memory whose 128-byte rows are swizzled.  K-major (rows of summed
 // indices): groups of eight rows are 1024 bytes apart.  MN-major (rows of kept indices, 64 a row): groups of eight
 // summed indices are 1024 bytes apart, the next 64 kept indices `chunk` bytes.

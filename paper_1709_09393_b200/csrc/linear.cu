@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     auto acc_empty = [&](uint32_t b) { return control + 144 + 8 * b; };
     const uint32_t slot = control + 160;
 
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
     const uint32_t group = blockIdx.x / CG, groups = gridDim.x / CG;
     const uint32_t items = args.tiles_m * args.tiles_n * args.splits;
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     bool ok = true;
     if (warp < kFirstEpilogueWarp) {
         if constexpr (kChunked<T, P>) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoaderRegs));
-        if (warp == 0 && lane == 0) {
+        if (warp == 0) {
             uint32_t s = 0, phase = 0;
             for (uint32_t item = group; item < items && ok; item += groups) {
                 uint32_t tm, tn;
@@ -273,29 +273,33 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         for (uint32_t kb = c0; kb < min(c0 + chunk, k1); ++kb) {
                             if (!(ok = mbar_wait(empty(s), phase ^ 1u))) break;
                             const uint32_t bar = CG == 2 ? cluster_addr(full(s), 0) : full(s);
-                            if (rank == 0) mbar_expect_tx(full(s), CG * S::stage);
                             const uint32_t a = base + s * S::stage, b = a + S::a_bytes;
                             const int32_t k = (int32_t)(kb * kBk);
                             const int32_t pa = kParts > 1 ? (int32_t)part_a(p) : 0, pb = kParts > 1 ? (int32_t)part_b(p) : 0;
-                            if constexpr (kMnA) {
+                            if (elect_one()) {
+                                if (rank == 0) mbar_expect_tx(full(s), CG * S::stage);
+                                if constexpr (kMnA) {
 #pragma unroll
-                                for (int c = 0; c < 2; ++c) tma_load<CG == 2>(a + c * 64 * kBk * 2, &map_a, row_a + c * 64, k, pa, bar);
-                            } else {
-                                tma_load<CG == 2>(a, &map_a, k, row_a, pa, bar);
-                            }
-                            if constexpr (kMnB) {
+                                    for (int c = 0; c < 2; ++c) tma_load<CG == 2>(a + c * 64 * kBk * 2, &map_a, row_a + c * 64, k, pa, bar);
+                                } else {
+                                    tma_load<CG == 2>(a, &map_a, k, row_a, pa, bar);
+                                }
+                                if constexpr (kMnB) {
 #pragma unroll
-                                for (int c = 0; c < BN / CG / 64; ++c) tma_load<CG == 2>(b + c * 64 * kBk * 2, &map_b, row_b + c * 64, k, pb, bar);
-                            } else {
-                                tma_load<CG == 2>(b, &map_b, k, row_b, pb, bar);
+                                    for (int c = 0; c < BN / CG / 64; ++c) tma_load<CG == 2>(b + c * 64 * kBk * 2, &map_b, row_b + c * 64, k, pb, bar);
+                                } else {
+                                    tma_load<CG == 2>(b, &map_b, k, row_b, pb, bar);
+                                }
                             }
+                            __syncwarp();
                             if (++s == S::stages) s = 0, phase ^= 1u;
                         }
             }
-        } else if (warp == 1 && lane == 0 && rank == 0) {
+        } else if (warp == 1 && rank == 0) {
             const uint32_t idesc = (1u << 4) | (args.format << 7) | (args.format << 10) | ((kMnA ? 1u : 0u) << 15) |
                                    ((kMnB ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 * CG >> 4) << 24);
             constexpr uint32_t step_a = (kMnA ? 2048u : 32u) >> 4, step_b = (kMnB ? 2048u : 32u) >> 4;
+            const uint32_t low_a = operand_desc_low(base, kMnA, 64 * kBk * 2), low_b = operand_desc_low(base + S::a_bytes, kMnB, 64 * kBk * 2);
             uint32_t s = 0, phase = 0, count = 0;
             for (uint32_t item = group; item < items && ok; item += groups) {
                 const uint32_t split = item % args.splits;
@@ -309,15 +313,18 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     for (uint32_t i = 0; i < steps; ++i) {
                         if (!(ok = mbar_wait(full(s), phase))) break;
                         tc_fence_after();
-                        const uint32_t a = base + s * S::stage, b = a + S::a_bytes;
-                        const uint64_t da = operand_desc(a, kMnA, 64 * kBk * 2), db = operand_desc(b, kMnB, 64 * kBk * 2);
+                        const uint32_t da = low_a + s * (S::stage >> 4), db = low_b + s * (S::stage >> 4);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int u = 0; u < kBk / 16; ++u)
-                            tc_mma<CG>(tmem + buf * BN, da + u * step_a, db + u * step_b, idesc, i > 0 || u > 0);
-                        tc_commit<CG>(empty(s));
+                            for (int u = 0; u < kBk / 16; ++u)
+                                tc_mma<CG>(tmem + buf * BN, operand_desc(da + u * step_a), operand_desc(db + u * step_b), idesc, i > 0 || u > 0);
+                            tc_commit<CG>(empty(s));
+                        }
+                        __syncwarp();
                         if (++s == S::stages) s = 0, phase ^= 1u;
                     }
-                    if (ok) tc_commit<CG>(acc_full(buf));
+                    if (ok && elect_one()) tc_commit<CG>(acc_full(buf));
+                    __syncwarp();
                 }
             }
         }

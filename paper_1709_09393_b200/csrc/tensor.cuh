@@ -14,6 +14,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 
+// One lane of a converged warp.  Code that a whole warp runs, with one lane chosen at the instruction itself, keeps its
+// operands in uniform registers; under `if (lane == 0)` each tcgen05 or TMA instruction waits for them to be moved there.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
 // The address, in the cluster's window, of `addr` in the CTA of rank `rank`.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     uint32_t r;
@@ -209,10 +217,15 @@ __device__ __forceinline__ void tmem_add16(uint32_t addr, float* v) {
 
 // Descriptor of an operand tile in shared memory whose 128-byte rows are swizzled.  K-major (rows of summed
 // indices): groups of eight rows are 1024 bytes apart.  MN-major (rows of kept indices, 64 a row): groups of eight
-// summed indices are 1024 bytes apart, the next 64 kept indices `chunk` bytes.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn_major, uint32_t chunk) {
-    const uint64_t lead = mn_major ? chunk >> 4 : 1u;
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+// summed indices are 1024 bytes apart, the next 64 kept indices `chunk` bytes.  The address is the low half's low part.
+__device__ __forceinline__ uint32_t operand_desc_low(uint32_t addr, bool mn_major, uint32_t chunk) {
+    return (addr >> 4) | (mn_major ? chunk >> 4 : 1u) << 16;
+}
+constexpr uint32_t kOperandDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint64_t operand_desc(uint32_t low) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(kOperandDescHigh));
+    return d;
 }
 
 }  // namespace slimdp

@@ -46,42 +46,61 @@ struct Extra {
     }
 };
 
-// V adjacent results C[i, j .. j + V), through the epilogue of product P; bias: the V values of these columns.
-template <typename T, Product P, int V>
-__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint64_t j, float (&v)[V], const float (&bias)[V],
-                                       const Extra<T, P, V>& x) {
+// B times V adjacent results C[i + b step, j .. j + V) for b < count, through the epilogue of product P, one step of it for all of
+// them at a time; bias: the V values of these columns.
+template <typename T, Product P, int V, int B>
+__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint32_t step, uint32_t count, uint64_t j, float (&v)[B][V],
+                                       const float (&bias)[V], const Extra<T, P, V> (&x)[B]) {
     if constexpr (P == kForward) {
 #pragma unroll
-        for (int c = 0; c < V; ++c) v[c] += bias[c];
-        if (e.z) store_pack<T, V>((T*)e.z + i * e.ldz + j, v);
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int c = 0; c < V; ++c) v[b][c] += bias[c];
+        if (e.z) {
+            T* const z = (T*)e.z + i * e.ldz + j;
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                if (b < count) store_pack<T, V>(z + (uint64_t)(b * step) * e.ldz, v[b]);
+        }
         with_act(e.act, [&](auto act) {
 #pragma unroll
-            for (int c = 0; c < V; ++c) v[c] = act_value<decltype(act)::value>(v[c]);
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] = act_value<decltype(act)::value>(v[b][c]);
         });
     } else if constexpr (P == kInput) {
         with_act(e.act, [&](auto act) {
-            float z[V];
-            unpack<T, V>(x.z, z);
 #pragma unroll
-            for (int c = 0; c < V; ++c) v[c] *= act_slope<decltype(act)::value>(z[c]);
+            for (int b = 0; b < B; ++b) {
+                float z[V];
+                unpack<T, V>(x[b].z, z);
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] *= act_slope<decltype(act)::value>(z[c]);
+            }
         });
     }
     if constexpr (P == kWeight) {
         if (e.accumulate) {
-            float old[V];
-            unpack<float, V>(x.old, old);
 #pragma unroll
-            for (int c = 0; c < V; ++c) v[c] += old[c];
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] += x[b].old.get(c);
         }
-        store_pack<float, V>((float*)e.out + i * e.ldo + j, v);
+        float* const out = (float*)e.out + i * e.ldo + j;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            if (b < count) store_pack<float, V>(out + (uint64_t)(b * step) * e.ldo, v[b]);
     } else {
         if (e.add) {
-            float a[V];
-            unpack<T, V>(x.add, a);
 #pragma unroll
-            for (int c = 0; c < V; ++c) v[c] += a[c];
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] += x[b].add.get(c);
         }
-        store_pack<T, V>((T*)e.out + i * e.ldo + j, v);
+        T* const out = (T*)e.out + i * e.ldo + j;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            if (b < count) store_pack<T, V>(out + (uint64_t)(b * step) * e.ldo, v[b]);
     }
 }
 
@@ -118,54 +137,53 @@ __device__ __forceinline__ void finish_rest(const ProductArgs& args, uint64_t i,
 #pragma unroll
     for (int c = 0; c < V; ++c)
         if (j + c < args.n) {
-            float one[1] = {v[c]}, b[1] = {P == kForward && args.e.bias ? __ldg(args.e.bias + j + c) : 0.0f};
-            Extra<T, P, 1> x;
-            x.load(args.e, i, j + c);
-            finish<T, P, 1>(args.e, i, j + c, one, b, x);
+            float one[1][1] = {{v[c]}}, b[1] = {P == kForward && args.e.bias ? __ldg(args.e.bias + j + c) : 0.0f};
+            Extra<T, P, 1> x[1];
+            x[0].load(args.e, i, j + c);
+            finish<T, P, 1, 1>(args.e, i, 0, 1, j + c, one, b, x);
         }
 }
 
 // A warp's 32 x 32 results, row-wise in shared memory: V adjacent columns a lane, so that a warp's accesses to memory
-// cover whole rows of the square; what the epilogue reads for BATCH such accesses is asked for at once.
+// cover whole rows of the square; B such accesses are made at once.
 template <typename T, Product P, int V, bool PARTIAL>
 __device__ __forceinline__ void finish_square_by(const ProductArgs& args, uint32_t split, const float* square,
                                                  uint64_t row0, uint64_t col0, uint32_t lane) {
-    constexpr int BATCH = V == 1 ? 8 : 4;
+    constexpr int B = V == 8 ? 4 : V == 4 ? 4 : 8;
     const uint32_t c = lane % (32 / V) * V, r = lane / (32 / V);
     const uint64_t j = col0 + c;
     if (j >= args.n || row0 >= args.m) return;
     const uint32_t rows = (uint32_t)min((uint64_t)32, args.m - row0);
-    if constexpr (PARTIAL) {
-        for (uint32_t k = r; k < rows; k += V) {
-            float v[V];
+    float bias[V];
 #pragma unroll
-            for (int u = 0; u < V; ++u) v[u] = square[k * kEpiloguePitch + c + u];
-            store_pack<float, V>(args.partial + ((uint64_t)split * args.m + row0 + k) * args.ld_partial + j, v);
-        }
-    } else {
-        float bias[V];
-#pragma unroll
-        for (int u = 0; u < V; ++u) bias[u] = P == kForward && args.e.bias && j + u < args.n ? __ldg(args.e.bias + j + u) : 0.0f;
-        const bool whole = j + V <= args.n;
+    for (int u = 0; u < V; ++u) bias[u] = !PARTIAL && P == kForward && args.e.bias && j + u < args.n ? __ldg(args.e.bias + j + u) : 0.0f;
+    const bool whole = PARTIAL || j + V <= args.n;
 #pragma unroll 1
-        for (uint32_t k0 = r; k0 < rows; k0 += V * BATCH) {
-            Extra<T, P, V> x[BATCH];
-            if (whole)
+    for (uint32_t k0 = r; k0 < rows; k0 += V * B) {
+        const uint64_t i = row0 + k0;
+        const uint32_t count = min((uint32_t)B, (rows - k0 + V - 1) / V);     // rows k0, k0 + V, ...
+        Extra<T, P, V> x[B];
+        if (!PARTIAL && whole) {
 #pragma unroll
-                for (int b = 0; b < BATCH; ++b)
-                    if (k0 + b * V < rows) x[b].load(args.e, row0 + k0 + b * V, j);
+            for (int b = 0; b < B; ++b)
+                if (b < count) x[b].load(args.e, i + b * V, j);
+        }
+        float v[B][V];
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) {
-                const uint32_t k = k0 + b * V;
-                if (k >= rows) break;
-                float v[V];
+        for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int u = 0; u < V; ++u) v[u] = square[k * kEpiloguePitch + c + u];
-                if (whole)
-                    finish<T, P, V>(args.e, row0 + k, j, v, bias, x[b]);
-                else
-                    finish_rest<T, P, V>(args, row0 + k, j, v);
-            }
+            for (int u = 0; u < V; ++u) v[b][u] = square[min(k0 + b * V, 31u) * kEpiloguePitch + c + u];
+        if constexpr (PARTIAL) {
+            float* const out = args.partial + ((uint64_t)split * args.m + i) * args.ld_partial + j;
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                if (b < count) store_pack<float, V>(out + (uint64_t)(b * V) * args.ld_partial, v[b]);
+        } else if (whole) {
+            finish<T, P, V, B>(args.e, i, V, count, j, v, bias, x);
+        } else {
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                if (b < count) finish_rest<T, P, V>(args, i + b * V, j, v[b]);
         }
     }
 }
@@ -244,6 +262,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
         mbar_init_fence();
     }
+    if constexpr (P == kWeight) allow_next_kernel();
     if (warp == 1) tmem_alloc<CG>(slot, S::columns);
     tc_fence_before();
     __syncthreads();
@@ -252,8 +271,6 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem + (slot - base));
 
-    // Sums of a chunked product take 128 registers of an epilogue warp: the first four warps give up theirs.  384 threads start
-    // with 168 each; 4 x 56 + 8 x 224 = 12 x 168 of a lane.
     bool ok = true;
     if (warp < kFirstEpilogueWarp) {
         if constexpr (kChunked<T, P>) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoaderRegs));
@@ -356,7 +373,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         tmem_add16(lanes + (count & 1u) * BN + q * 16, &sum[q / 2][q % 2 * 16]);
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(cluster_addr(acc_empty(count & 1u), 0));
+                    if (lane == 0) mbar_arrive_read(cluster_addr(acc_empty(count & 1u), 0));
                 }
                 if (!ok) break;
 #pragma unroll 1
@@ -385,7 +402,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     }
                     if (q == kSquares - 1) tc_fence_before();      // the accumulator has been read
                     __syncwarp();
-                    if (q == kSquares - 1 && lane == 0) mbar_arrive_cluster(cluster_addr(acc_empty(buf), 0));
+                    if (q == kSquares - 1 && lane == 0) mbar_arrive_read(cluster_addr(acc_empty(buf), 0));
                     finish_square<T, P>(args, split, square, row0, col0 + q * 32, lane);
                     __syncwarp();
                 }
@@ -406,34 +423,68 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if constexpr (CG == 2) cluster_sync();      // neither CTA of a pair leaves before both have freed
 }
 
-// Joins the sums of `splits` parts of the summed axis and finishes them.
-template <typename T, Product P, int V>
+// Joins the sums of `splits` parts of the summed axis and finishes them: 256 / W places a CTA, each of W warps adds every W-th part of
+// them, and the first finishes the sums of the W, in a fixed order.  Bound by reading the partial sums; eight warps a place
+// where there are eight parts or more, which one thread would read one after the other.
+template <typename T, Product P, int V, int W>
 __global__ void __launch_bounds__(256) join_kernel(const ProductArgs args) {
+    constexpr int PLACES = 256 / W;
+    __shared__ float sums[W][V][PLACES];
+    const uint32_t place = threadIdx.x % PLACES, part = threadIdx.x / PLACES;
     const uint64_t pieces = (args.n + V - 1) / V, total = pieces * args.m;
-    for (uint64_t p = (uint64_t)blockIdx.x * 256 + threadIdx.x; p < total; p += (uint64_t)gridDim.x * 256) {
-        const uint64_t i = p / pieces, j = (p - i * pieces) * V;
-        float v[V] = {};
-        for (uint32_t s = 0; s < args.splits; ++s) {
-            const float* src = args.partial + ((uint64_t)s * args.m + i) * args.ld_partial + j;
+    for (uint64_t p0 = (uint64_t)blockIdx.x * PLACES; p0 < total; p0 += (uint64_t)gridDim.x * PLACES) {
+        const uint64_t p = p0 + place, i = p / pieces, j = (p - i * pieces) * V;
+        float v[1][V] = {};
+        if (p < total) {
+#pragma unroll 4
+            for (uint32_t s = part; s < args.splits; s += W) {
+                const float* src = args.partial + ((uint64_t)s * args.m + i) * args.ld_partial + j;
 #pragma unroll
-            for (int c = 0; c < V; ++c) v[c] += src[c];       // ld_partial is a multiple of V: in bounds
+                for (int c = 0; c < V; ++c) v[0][c] += src[c];       // ld_partial is a multiple of V: in bounds
+            }
         }
-        if (j + V > args.n) {
-            finish_rest<T, P, V>(args, i, j, v);
-            continue;
-        }
-        float bias[V];
+        if constexpr (W > 1) {
 #pragma unroll
-        for (int c = 0; c < V; ++c) bias[c] = P == kForward && args.e.bias ? __ldg(args.e.bias + j + c) : 0.0f;
-        Extra<T, P, V> x;
-        x.load(args.e, i, j);
-        finish<T, P, V>(args.e, i, j, v, bias, x);
+            for (int c = 0; c < V; ++c) sums[part][c][place] = v[0][c];
+            __syncthreads();
+            if (part == 0)
+#pragma unroll
+                for (int w = 1; w < W; ++w)
+#pragma unroll
+                    for (int c = 0; c < V; ++c) v[0][c] += sums[w][c][place];
+        }
+        if (part == 0 && p < total) {
+            if (j + V > args.n) {
+                finish_rest<T, P, V>(args, i, j, v[0]);
+            } else {
+                float bias[V];
+#pragma unroll
+                for (int c = 0; c < V; ++c) bias[c] = P == kForward && args.e.bias ? __ldg(args.e.bias + j + c) : 0.0f;
+                Extra<T, P, V> x[1];
+                x[0].load(args.e, i, j);
+                finish<T, P, V, 1>(args.e, i, 0, 1, j, v, bias, x);
+            }
+        }
+        if constexpr (W > 1) __syncthreads();
     }
+}
+
+template <typename T, Product P, int V>
+slimdp_status launch_join(const ProductArgs& args, cudaStream_t st) {
+    const uint64_t places = (args.n + V - 1) / V * args.m, most = (uint64_t)sm_count() * 8;
+    if (args.splits >= 8)
+        join_kernel<T, P, V, 8><<<(unsigned)std::min<uint64_t>((places + 31) / 32, most), 256, 0, st>>>(args);
+    else
+        join_kernel<T, P, V, 1><<<(unsigned)std::min<uint64_t>((places + 255) / 256, most), 256, 0, st>>>(args);
+    SLIMDP_LAUNCHED(1);
+    return SLIMDP_OK;
 }
 
 // db (+)= sum over rows of dy.  A cluster of eight CTAs takes 32 V columns, each of its 256 warps every 256th row; sums go from
 // registers to shared memory to rank 0, in a fixed order.  Bound by reading dy: 32 warps with eight 16-byte loads a
-// thread in flight keep an SM's share of the bandwidth busy.
+// thread in flight keep an SM's share of the bandwidth busy.  It is launched after the weight's product and may start beside it, on
+// SMs that have no tile or no tile left, for it needs nothing of it; it ends after it, so that what follows waits for both.
+// Sums inside the product, from its stages in shared memory, cost the tiles that made them more than this kernel takes.
 constexpr uint32_t kSumRanks = 8, kSumWarps = 32;
 constexpr int kSumAhead = 8;
 
@@ -488,6 +539,26 @@ __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWar
             db[col] = accumulate ? db[col] + t : t;
         }
     cluster_sync();             // no CTA leaves while its sums are read
+    wait_for_last_kernel();
+}
+
+template <typename T>
+slimdp_status launch_column_sum(const T* dy, uint64_t lddy, uint64_t m, uint64_t n, float* db, bool accumulate, cudaStream_t st) {
+    const bool wide = aligned16(dy) && (lddy * sizeof(T)) % 16 == 0;
+    const uint64_t columns = wide ? 32 * kVec<T> : 32;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((n + columns - 1) / columns) * kSumRanks);
+    cfg.blockDim = dim3(32 * kSumWarps);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, wide ? column_sum_kernel<T, kVec<T>> : column_sum_kernel<T, 1>, dy, lddy, m, n, db, accumulate) != cudaSuccess)
+        return SLIMDP_ERR_CUDA;
+    SLIMDP_LAUNCHED(1);
+    return SLIMDP_OK;
 }
 
 template <typename T>
@@ -679,25 +750,39 @@ struct Plan {
 
 uint64_t partial_bytes(uint64_t m, uint64_t n) { return m * align_up(n, 8) * 4; }
 
-Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks) {
+// The cut with the least estimated time, in ns, from what was measured on one B200.  A stage of 64 summed indices takes a CTA as long
+// as its products (2 cycles a column at 1.9 GHz) or as its bytes at 110 a ns, the rate at which L2 feeds an SM while all
+// ask, and 180 at least; a tile's epilogue that nothing follows 600 and 350 more for each 64 columns.  A split adds a second kernel that reads
+// the partial sums (2500, and 5000 bytes a ns).  Large products end with 256 x 256, whose stage is bound by its products.
+Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts) {
     const uint64_t sms = 148;
-    Plan p = {2, 256, 1};
-    const uint64_t big = ((m + 255) / 256) * ((n + 255) / 256);
-    if (big * 2 <= sms / 2 || m <= 128) p = {1, n > 64 && ((m + 127) / 128) * ((n + 127) / 128) >= sms ? 128u : 64u, 1};
-    const uint64_t tiles = ((m + 128 * p.pair - 1) / (128 * p.pair)) * ((n + p.width - 1) / p.width);
-    const uint64_t slots = sms / p.pair;
-    if (tiles * 2 <= slots) {
-        uint64_t s = std::min(slots / tiles, std::max<uint64_t>(kblocks / 4, 1));
-        s = std::min(s, kPartialBytes / partial_bytes(m, n));
-        if (s > 1) p.splits = (uint32_t)s;
+    Plan best = {};
+    double least = 0.0;
+    for (const Plan shape : {Plan{2, 256, 1}, Plan{2, 128, 1}, Plan{1, 128, 1}, Plan{1, 64, 1}}) {
+        const uint64_t tiles = ((m + 128 * shape.pair - 1) / (128 * shape.pair)) * ((n + shape.width - 1) / shape.width);
+        const uint64_t slots = sms / shape.pair;
+        const double bytes = 128.0 * (std::min<uint64_t>(m, 128) + std::min<uint64_t>(n, shape.width / shape.pair));
+        const double stage = std::max({2.0 * shape.width / 1.9, bytes / 110.0, 180.0});
+        uint64_t most = tiles * 2 <= slots ? std::min(slots / tiles, std::max<uint64_t>(kblocks / 4, 1)) : 1;
+        most = std::max<uint64_t>(1, std::min(most, kPartialBytes / partial_bytes(m, n)));
+        for (uint64_t splits : {uint64_t(1), most}) {
+            const double waves = (double)((tiles * splits + slots - 1) / slots), steps = (double)((kblocks + splits - 1) / splits * parts);
+            double t = waves * steps * stage + 600.0 + 350.0 * shape.width / 64;
+            if (splits > 1) t += 2500.0 + (double)(splits * partial_bytes(m, n)) / 5000.0;
+            if (best.pair == 0 || t < least) {
+                least = t;
+                best = {shape.pair, shape.width, (uint32_t)splits};
+            }
+        }
     }
-    return p;
+    return best;
 }
 
 // C [m, n] = sum over k; a and b hold k along their rows or, where they are MN-major, along their columns.
 template <typename T, Product P>
 slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_t k, const Epilogue& e, Scratch ws,
-                             cudaStream_t st) {
+                             cudaStream_t st, float* db = nullptr) {
+    const Matrix dy = a;
     constexpr bool kMnA = P == kWeight, kMnB = P != kForward, kF16 = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value;
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
     slimdp_status s = prepare_operands<T>(a, b, ws, st);
@@ -711,7 +796,7 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
     const uint64_t size = P == kWeight ? 4 : sizeof(T);
     auto starts_wide = [&](const void* p, uint64_t ld) { return !p || (aligned16(p) && (ld * size) % 16 == 0); };
     args.wide = starts_wide(e.out, e.ldo) && starts_wide(e.z, e.ldz) && starts_wide(e.add, e.ldadd);
-    const Plan plan = plan_product(m, n, args.kblocks);
+    const Plan plan = plan_product(m, n, args.kblocks, kParts == 3 ? 6 : 1);
     args.splits = plan.splits;
     args.tiles_m = (uint32_t)((m + 128 * plan.pair - 1) / (128 * plan.pair));
     args.tiles_n = (uint32_t)((n + plan.width - 1) / plan.width);
@@ -726,22 +811,17 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
     const int sms = sm_count();
     if (sms <= 0) return SLIMDP_ERR_CUDA;
     const uint32_t groups = std::min<uint32_t>(items, (uint32_t)sms / plan.pair);
-    if (plan.pair == 2)
+    if (plan.pair == 2 && plan.width == 256)
         s = launch_tiles<T, P, 2, 256>(map_a, map_b, args, groups, st);
+    else if (plan.pair == 2)
+        s = launch_tiles<T, P, 2, 128>(map_a, map_b, args, groups, st);
     else if (plan.width == 128)
         s = launch_tiles<T, P, 1, 128>(map_a, map_b, args, groups, st);
     else
         s = launch_tiles<T, P, 1, 64>(map_a, map_b, args, groups, st);
+    if (s == SLIMDP_OK && db) s = launch_column_sum<T>((const T*)dy.p, dy.ld, dy.rows, dy.cols, db, e.accumulate, st);
     if (s != SLIMDP_OK || args.splits == 1) return s;
-    constexpr int V = kWide<T, P>;
-    const uint64_t pieces = (args.wide ? (n + V - 1) / V : n) * m;
-    const unsigned ctas = (unsigned)std::min<uint64_t>((pieces + 255) / 256, (uint64_t)sms * 8);
-    if (args.wide)
-        join_kernel<T, P, V><<<ctas, 256, 0, st>>>(args);
-    else
-        join_kernel<T, P, 1><<<ctas, 256, 0, st>>>(args);
-    SLIMDP_LAUNCHED(1);
-    return SLIMDP_OK;
+    return args.wide ? launch_join<T, P, kWide<T, P>>(args, st) : launch_join<T, P, 1>(args, st);
 }
 
 }  // namespace
@@ -749,9 +829,9 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
 size_t linear_ws_bytes(uint64_t m, uint64_t n, uint64_t k, int32_t type) {
     // two packed operands and the partial sums of a split, of whichever of the three products takes most
     const uint64_t x = packed_bytes(m, k, type), w = packed_bytes(n, k, type), dy = packed_bytes(m, n, type);
-    auto partial = [](uint64_t rows, uint64_t cols, uint64_t summed) -> uint64_t {
+    auto partial = [&](uint64_t rows, uint64_t cols, uint64_t summed) -> uint64_t {
         if (rows == 0 || summed == 0) return 0;
-        const Plan p = plan_product(rows, cols, (summed + kBk - 1) / kBk);
+        const Plan p = plan_product(rows, cols, (summed + kBk - 1) / kBk, type == SLIMDP_F32 ? 6 : 1);
         return p.splits > 1 ? align_up(p.splits * partial_bytes(rows, cols), 256) : 0;
     };
     return 256 + std::max({x + w + partial(m, n, k), dy + w + partial(m, k, n), dy + x + partial(n, k, m)});
@@ -793,19 +873,11 @@ slimdp_status launch_linear_backward_weight(const void* dy, uint64_t lddy, const
     const Epilogue e = {nullptr, nullptr, 0, nullptr, 0, dw, lddw, SLIMDP_ACT_NONE, accumulate};
     return with_type(type, [&](auto v) -> slimdp_status {
         using T = decltype(v);
-        if (db) {
-            const bool wide = aligned16(dy) && (lddy * sizeof(T)) % 16 == 0;
-            const uint64_t columns = wide ? 32 * kVec<T> : 32;
-            const unsigned ctas = (unsigned)((n + columns - 1) / columns) * kSumRanks;
-            if (wide)
-                column_sum_kernel<T, kVec<T>><<<ctas, 32 * kSumWarps, 0, st>>>((const T*)dy, lddy, m, n, db, accumulate);
-            else
-                column_sum_kernel<T, 1><<<ctas, 32 * kSumWarps, 0, st>>>((const T*)dy, lddy, m, n, db, accumulate);
-            SLIMDP_LAUNCHED(1);
-        }
-        if (m == 0)
+        if (m == 0) {
+            if (db && cudaMemsetAsync(db, 0, n * 4, st) != cudaSuccess) return SLIMDP_ERR_CUDA;
             return cudaMemset2DAsync(dw, lddw * 4, 0, k * 4, n, st) == cudaSuccess ? SLIMDP_OK : SLIMDP_ERR_CUDA;
-        return launch_product<T, kWeight>({dy, lddy, m, n}, {x, ldx, m, k}, n, k, m, e, Scratch{(uint8_t*)ws}, st);
+        }
+        return launch_product<T, kWeight>({dy, lddy, m, n}, {x, ldx, m, k}, n, k, m, e, Scratch{(uint8_t*)ws}, st, db);
     });
 }
 

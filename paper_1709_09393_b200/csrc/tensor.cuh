@@ -49,9 +49,11 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Arrives at a barrier of any CTA of the cluster (an address made by cluster_addr).
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// Arrives at a barrier of any CTA of the cluster (an address made by cluster_addr) to say that what was read from tensor memory is in
+// registers.  Relaxed: nothing in memory is handed over, and a release would wait for all stores of the warp before it, which
+// are the results of the last tile on their way to memory.
+__device__ __forceinline__ void mbar_arrive_read(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
@@ -131,6 +133,11 @@ __device__ __forceinline__ uint32_t cluster_size() {
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
+
+// Lets the next kernel of the stream start, where it was launched so, as soon as SMs are free; and waits, in that next kernel, until
+// the one before is complete.
+__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // ---- tcgen05; CG = 2: the two CTAs of a pair work on one tile
 

@@ -333,14 +333,19 @@ __host__ __device__ inline uint32_t table_slots(uint32_t top) {
     return n;
 }
 
+// Rows whose exchange and entries are kept at a time.  Entries of row r + 4 are sent to rank 0 when the slice of row r + 4 is there,
+// which is asked for when the exchange of row r + 2 is complete, which rank 0's dense warps are part of once their slice of
+// row r + 2 is there, which is asked for when the loss of row r has been read: with four, nothing is overwritten unread.
+constexpr uint32_t kTurns = 4;
+
 template <typename T, int WARPS, int PIECES>
 struct SliceShape {
     static constexpr int elems = PIECES * kVec<T>;                       // of a thread
     static constexpr uint32_t pieces = 32 * WARPS * PIECES, bytes = pieces * 16;
     static constexpr uint32_t said = 8 * WARPS * kVoice + 8 * kFacts + kOwn;            // floats of an exchange
-    static constexpr uint32_t control = 3 * said * 4 + 128 + 3 * kNote * 4;
-    // of an entry of the teacher: index, logit, q and the student's logit, for three rows
-    static uint32_t smem(uint32_t top) { return 2 * bytes + control + top * 3 * 16 + table_slots(top) * 4; }
+    static constexpr uint32_t control = kTurns * said * 4 + 128 + kTurns * kNote * 4;
+    // of an entry of the teacher: index, logit, q and the student's logit
+    static uint32_t smem(uint32_t top) { return 2 * bytes + control + top * kTurns * 16 + table_slots(top) * 4; }
 };
 
 // The part of a row's 16-byte pieces that a CTA holds, and the single elements before and after the pieces.
@@ -408,18 +413,18 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
     constexpr int V = kVec<T>, kDense = 32 * WARPS;
     extern __shared__ __align__(128) uint8_t smem[];
     T* const slice = reinterpret_cast<T*>(smem);                                   // [2][pieces * V]
-    float* const exchange = reinterpret_cast<float*>(smem + 2 * S::bytes);         // [3][said]
-    const uint32_t bars = smem_addr(exchange + 3 * S::said);
-    float* const notes = exchange + 3 * S::said + 32;                              // [3][kNote]
-    int32_t* const all_idx = reinterpret_cast<int32_t*>(smem + 2 * S::bytes + S::control);   // [3][top] each
-    float* const all_t = reinterpret_cast<float*>(all_idx + 3 * a.top);
-    float* const all_q = all_t + 3 * a.top;
-    float* const all_z = all_q + 3 * a.top;
-    int32_t* const table = reinterpret_cast<int32_t*>(all_z + 3 * a.top);
+    float* const exchange = reinterpret_cast<float*>(smem + 2 * S::bytes);         // [kTurns][said]
+    const uint32_t bars = smem_addr(exchange + kTurns * S::said);
+    float* const notes = exchange + kTurns * S::said + 32;                         // [kTurns][kNote]
+    int32_t* const all_idx = reinterpret_cast<int32_t*>(smem + 2 * S::bytes + S::control);   // [kTurns][top] each
+    float* const all_t = reinterpret_cast<float*>(all_idx + kTurns * a.top);
+    float* const all_q = all_t + kTurns * a.top;
+    float* const all_z = all_q + kTurns * a.top;
+    int32_t* const table = reinterpret_cast<int32_t*>(all_z + kTurns * a.top);
     auto full = [&](uint32_t turn) { return bars + 8 * (turn & 1u); };
     auto done = [&](uint32_t turn) { return bars + 16 + 8 * (turn & 1u); };
     auto handed = [&](uint32_t turn) { return bars + 32 + 8 * (turn & 1u); };
-    auto told = [&](uint32_t third) { return bars + 48 + 8 * third; };
+    auto told = [&](uint32_t turn) { return bars + 48 + 8 * (turn % kTurns); };
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t ranks = cluster_size(), rank = cluster_rank(), ranks_log2 = __ffs(ranks) - 1;   // a power of two
     const uint32_t first = blockIdx.x >> ranks_log2, step = gridDim.x >> ranks_log2;
@@ -431,14 +436,14 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
             mbar_init(done(i), WARPS);
             mbar_init(handed(i), 1);
         }
-        for (int i = 0; i < 3; ++i) mbar_init(told(i), 1);
+        for (uint32_t i = 0; i < kTurns; ++i) mbar_init(told(i), 1);
         mbar_init_fence();
     }
     __syncthreads();
     cluster_sync();             // every CTA of the cluster runs and has its barriers
 
     bool ok = true;
-    uint32_t turn = 0, third = 0, thirds = 0;         // row `turn` exchanges through buffer `third` for the `thirds`-th time
+    uint32_t turn = 0;
     if (warp < WARPS) {
         for (uint64_t row = first; row < a.rows; row += step, ++turn) {
             const T* const z = logits + row * a.ldl;
@@ -511,15 +516,14 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
             }
             sum_t = warp_sum(sum_t);
             if constexpr (SECOND) sum_1 = warp_sum(sum_1);
-            float* const said = exchange + third * S::said;
+            float* const said = exchange + turn % kTurns * S::said;
             if (lane < ranks)
                 send_cluster(cluster_addr(smem_addr(said + (rank * WARPS + warp) * kVoice), lane), m_w, sum_t, sum_1, 0.0f,
-                             cluster_addr(told(third), lane));
-            if (!(ok = mbar_wait(told(third), thirds & 1u))) break;
+                             cluster_addr(told(turn), lane));
+            if (!(ok = mbar_wait(told(turn), (turn / kTurns) & 1u))) break;
             float m;
             row_sums<SECOND>(said, voices, lane, c, c_1, m, sum_t, sum_1);
             const float* const own = said + 8 * WARPS * kVoice + 8 * kFacts;
-            if (++third == 3) third = 0, ++thirds;
             if (out) {
                 const float coef_t = own[kCoefT], coef_1 = own[kCoef1];
                 // a row without a term, or with nothing but -inf, has gradient 0, whatever it holds
@@ -613,13 +617,13 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
             const float w = next_w;
             const int32_t y = next_y;
             const bool has_label = a.ce != 0.0f && y >= 0 && (uint32_t)y < a.vocab, label_mine = has_label && mine(y);
-            int32_t* const s_idx = all_idx + third * a.top;               // -1: not in this slice
-            float *const s_t = all_t + third * a.top, *const s_q = all_q + third * a.top, *const s_z = all_z + third * a.top;
-            float* const note = notes + third * kNote;
-            float* const said = exchange + third * S::said;
+            int32_t* const s_idx = all_idx + turn % kTurns * a.top;               // -1: not in this slice
+            float *const s_t = all_t + turn % kTurns * a.top, *const s_q = all_q + turn % kTurns * a.top, *const s_z = all_z + turn % kTurns * a.top;
+            float* const note = notes + turn % kTurns * kNote;
+            float* const said = exchange + turn % kTurns * S::said;
             float* const facts = said + 8 * WARPS * kVoice;
             if (front) {
-                // the slice's arrival also says that the entries of three rows ago are done with
+                // the slice's arrival also says that the entries of kTurns rows ago are done with
                 if (!(ok = mbar_wait(full(turn), (turn >> 1) & 1u))) break;
                 const T* const held = slice + (turn & 1u) * S::pieces * V;
                 auto value = [&](uint32_t i) { return i >= from && i < to ? to_f32(held[i - from]) : to_f32(z[i]); };
@@ -660,10 +664,10 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
                 total = warp_sum(total), sum_q = warp_sum(sum_q), term = warp_sum(term);
                 const float per = 1.0f / total;
                 if (lane == 0) {
-                    mbar_expect_tx(told(third), voices * kVoice * 4 + kOwn * 4 + (rank == 0 ? ranks * kFacts * 4 : 0));
+                    mbar_expect_tx(told(turn), voices * kVoice * 4 + kOwn * 4 + (rank == 0 ? ranks * kFacts * 4 : 0));
                     send_cluster(cluster_addr(smem_addr(facts + 8 * kFacts), rank), has_teacher ? w * a.kd * a.temperature : 0.0f,
-                                 has_label ? w * a.ce : 0.0f, 0.0f, 0.0f, cluster_addr(told(third), rank));
-                    const uint32_t dst = cluster_addr(smem_addr(facts + rank * kFacts), 0), bar = cluster_addr(told(third), 0);
+                                 has_label ? w * a.ce : 0.0f, 0.0f, 0.0f, cluster_addr(told(turn), rank));
+                    const uint32_t dst = cluster_addr(smem_addr(facts + rank * kFacts), 0), bar = cluster_addr(told(turn), 0);
                     send_cluster(dst, base, has_teacher ? sum_q * per : 0.0f, has_teacher ? term * per : 0.0f, label_mine ? 1.0f : 0.0f, bar);
                     send_cluster(dst + 16, z_label, 0.0f, 0.0f, 0.0f, bar);
                     note[kNoteTotal] = total;
@@ -671,8 +675,7 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(handed(turn));
-                if (++third == 3) third = 0, ++thirds;
-                continue;
+                    continue;
             }
             fetch(row + step);
             if (!(ok = mbar_wait(handed(turn), (turn >> 1) & 1u))) break;
@@ -708,7 +711,7 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
                 }
                 __syncwarp();
             }
-            if (!(ok = mbar_wait(told(third), thirds & 1u))) break;
+            if (!(ok = mbar_wait(told(turn), (turn / kTurns) & 1u))) break;
             float m, sum_t, sum_1;
             row_sums<SECOND>(said, voices, lane, c, c_1, m, sum_t, sum_1);
             const float coef_t = facts[8 * kFacts + kCoefT], coef_1 = facts[8 * kFacts + kCoef1];
@@ -730,7 +733,6 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
                 if (has_label) loss += a.ce * (log_sum(sum_1, m, SECOND == kOwnSecond ? c_1 : c, SECOND > kOwnSecond ? SECOND : 1) - label);
                 if (lane == 0) a.loss[row] = none ? 0.0f : w * loss;
             }
-            if (++third == 3) third = 0, ++thirds;
             // 2^((s - m) c) relative to the sums as they are kept
             const float abs_t = (SECOND ? coef_t : coef_t + coef_1) / sum_t * exp2_approx(fabsf(m) < kFar ? fmaf(m, c, -ceilf(m * c)) : 0.0f);
             const float abs_1 = SECOND ? coef_1 / sum_1 * exp2_approx(fabsf(m) < kFar ? fmaf(m, c_1, -reference_1<SECOND>(m, c, c_1)) : 0.0f) : 0.0f;

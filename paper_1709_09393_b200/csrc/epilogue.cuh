@@ -1,0 +1,106 @@
+// What follows a matrix product of a layer, shared by the kernels that make the products.
+#pragma once
+
+#include "train.cuh"
+
+namespace slimdp {
+
+// What is done with C[i, j] before it is stored; NULL members are left out.
+struct Epilogue {
+    const float* bias;                 // + bias[j]
+    void* z;  uint64_t ldz;            // pre-activation: written by forward, read by backward_input
+    const void* add;  uint64_t ldadd;  // residual or its gradient
+    void* out;  uint64_t ldo;
+    int act;
+    bool accumulate;                   // out is fp32 and keeps what it holds
+};
+
+enum Product { kForward, kInput, kWeight };
+
+// Most rows that the ordinary cores multiply, forward.
+constexpr uint64_t kFewRows = 8;
+
+// Whether they are to be preferred to the tensor cores, whose tiles of 128 rows would be all but empty: estimated times in us.  Measured
+// on one B200, bf16: one row of 4096 x 4096 5.1 against 13.4, five rows of 4096 x 1024 6.3 against 8.8, eight rows of
+// 16384 x 4096 67 against 27.
+inline bool few_rows(uint64_t m, uint64_t n, uint64_t k) {
+    const double rows = m <= 2 ? (double)m : m <= 4 ? 4.0 : 8.0, weight = (double)n * (double)k;
+    return m <= kFewRows && 2.0 + rows * weight / 8e6 < 9.0 + weight / 3e6;
+}
+
+// What the epilogue reads at V adjacent results: loaded for several places at once, before any of them is worked on.
+template <typename T, Product P, int V>
+struct Extra {
+    Pack<T, V> z, add;
+    Pack<float, V> old;
+
+    __device__ __forceinline__ void load(const Epilogue& e, uint64_t i, uint64_t j) {
+        if constexpr (P == kInput)
+            if (e.act != SLIMDP_ACT_NONE) z = load_pack<T, V>((const T*)e.z + i * e.ldz + j);
+        if constexpr (P == kWeight) {
+            if (e.accumulate) old = load_pack<float, V>((const float*)e.out + i * e.ldo + j);
+        } else {
+            if (e.add) add = load_pack<T, V>((const T*)e.add + i * e.ldadd + j);
+        }
+    }
+};
+
+// B times V adjacent results C[i + b step, j .. j + V) for b < count, through the epilogue of product P, one step of it for all of
+// them at a time; bias: the V values of these columns.
+template <typename T, Product P, int V, int B>
+__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint32_t step, uint32_t count, uint64_t j, float (&v)[B][V],
+                                       const float (&bias)[V], const Extra<T, P, V> (&x)[B]) {
+    if constexpr (P == kForward) {
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int c = 0; c < V; ++c) v[b][c] += bias[c];
+        if (e.z) {
+            T* const z = (T*)e.z + i * e.ldz + j;
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                if (b < count) store_pack<T, V>(z + (uint64_t)(b * step) * e.ldz, v[b]);
+        }
+        with_act(e.act, [&](auto act) {
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] = act_value<decltype(act)::value>(v[b][c]);
+        });
+    } else if constexpr (P == kInput) {
+        with_act(e.act, [&](auto act) {
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                float z[V];
+                unpack<T, V>(x[b].z, z);
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] *= act_slope<decltype(act)::value>(z[c]);
+            }
+        });
+    }
+    if constexpr (P == kWeight) {
+        if (e.accumulate) {
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] += x[b].old.get(c);
+        }
+        float* const out = (float*)e.out + i * e.ldo + j;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            if (b < count) store_pack<float, V>(out + (uint64_t)(b * step) * e.ldo, v[b]);
+    } else {
+        if (e.add) {
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[b][c] += x[b].add.get(c);
+        }
+        T* const out = (T*)e.out + i * e.ldo + j;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            if (b < count) store_pack<T, V>(out + (uint64_t)(b * step) * e.ldo, v[b]);
+    }
+}
+
+}  // namespace slimdp

@@ -1,0 +1,138 @@
+// The forward product of up to eight rows, as single tokens make it, on the ordinary cores.
+//
+// Bound by reading w [n, k] once: warps walk over its rows in 16-byte pieces, the rows of x stay in L1.  fp32 is multiplied as it
+// is.  Sums run over the summed axis in a fixed order, so that results do not depend on scheduling.
+#include <algorithm>
+
+#include "epilogue.cuh"
+
+namespace slimdp {
+
+namespace {
+
+constexpr int kColumns = 4;            // outputs of a warp, forward
+
+// N sums over a warp, N a power of two: value i ends in every lane l with l % N = i.  Halves are exchanged and added, N - 1
+// exchanges and log2(32 / N) more instead of 5 N.
+template <int N>
+__device__ __forceinline__ float warp_sums(float (&v)[N], uint32_t lane) {
+#pragma unroll
+    for (int d = N / 2; d >= 1; d >>= 1) {
+        const bool upper = lane & d;
+#pragma unroll
+        for (int i = 0; i < d; ++i) {
+            const float keep = upper ? v[i + d] : v[i], send = upper ? v[i] : v[i + d];
+            v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, d);
+        }
+    }
+#pragma unroll
+    for (int d = N; d < 32; d <<= 1) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], d);
+    return v[0];
+}
+
+// y = act(x w^T + bias) + residual: a warp makes M x 4 dot products over every (1 << split)-th stretch of 32 pieces; the warps
+// of a CTA that share outputs add theirs.  16-byte pieces where the rows allow, else single elements.
+template <typename T, int V, int M>
+__global__ void __launch_bounds__(256) few_forward_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w,
+                                                          uint64_t ldw, uint32_t m, uint64_t n, uint64_t k, uint32_t split,
+                                                          const Epilogue e) {
+    constexpr int N = M * kColumns;
+    __shared__ float sums[8][N];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ways = 1u << split, way = warp & (ways - 1);
+    const uint64_t j0 = ((uint64_t)blockIdx.x * (8 >> split) + (warp >> split)) * kColumns;
+    const T *wr[kColumns], *xr[M];
+#pragma unroll
+    for (int c = 0; c < kColumns; ++c) wr[c] = w + min(j0 + c, n - 1) * ldw;       // a row beyond the last is not stored
+#pragma unroll
+    for (int i = 0; i < M; ++i) xr[i] = x + min((uint32_t)i, m - 1) * ldx;
+    // sums of the even and of the odd elements; more of them would not fit the registers of eight rows
+    using Acc = Vals<V == 1 ? 1 : 2>;
+    Acc acc[M][kColumns];
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) acc[i][c] = Acc::splat(0.0f);
+    const uint64_t pieces = k / V;
+#pragma unroll 2
+    for (uint64_t p = way * 32 + lane; p < pieces; p += ways * 32) {
+        Vals<V> a[kColumns];
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) a[c] = Vals<V>::of(load_pack<T, V>(wr[c] + p * V));
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const Vals<V> b = Vals<V>::of(load_pack<T, V>(xr[i] + p * V));
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c)
+#pragma unroll
+                for (int u = 0; u < (V + 1) / 2; ++u) acc[i][c].p[0] = fma_pair(a[c].p[u], b.p[u], acc[i][c].p[0]);
+        }
+    }
+    float v[N];
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) v[i * kColumns + c] = acc[i][c].sum();
+    if (V > 1 && way == 0 && pieces * V + lane < k) {
+        const uint64_t l = pieces * V + lane;
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) v[i * kColumns + c] = fmaf(to_f32(xr[i][l]), to_f32(wr[c][l]), v[i * kColumns + c]);
+    }
+    const float s = warp_sums<N>(v, lane);
+    if (lane < N) sums[warp][lane] = s;
+    __syncthreads();
+    if (way != 0 || lane >= N) return;
+    float one[1][1] = {{s}};
+    for (uint32_t o = 1; o < ways; ++o) one[0][0] += sums[warp + o][lane];
+    const uint64_t i = lane / kColumns, j = j0 + lane % kColumns;
+    if (i >= m || j >= n) return;
+    const float bias[1] = {e.bias ? __ldg(e.bias + j) : 0.0f};
+    Extra<T, kForward, 1> extra[1];
+    extra[0].load(e, i, j);
+    finish<T, kForward, 1, 1>(e, i, 0, 1, j, one, bias, extra);
+}
+
+// Calls f with the smallest of 1, 2, 4 and 8 that is not below m, as a constant.
+template <typename F>
+slimdp_status with_rows(uint64_t m, F&& f) {
+    if (m <= 1) return f(std::integral_constant<int, 1>());
+    if (m <= 2) return f(std::integral_constant<int, 2>());
+    if (m <= 4) return f(std::integral_constant<int, 4>());
+    return f(std::integral_constant<int, 8>());
+}
+
+static_assert(kFewRows == 8, "with_rows covers all");
+
+}  // namespace
+
+template <typename T>
+slimdp_status launch_few_forward(const T* x, uint64_t ldx, const T* w, uint64_t ldw, uint64_t m, uint64_t n, uint64_t k,
+                                 const Epilogue& e, cudaStream_t st) {
+    const bool wide = aligned16(x) && aligned16(w) && (ldw * sizeof(T)) % 16 == 0 && (m == 1 || (ldx * sizeof(T)) % 16 == 0);
+    const uint64_t warps = (n + kColumns - 1) / kColumns, stretches = (wide ? k / kVec<T> : k) / 32;
+    const int sms = sm_count();
+    if (sms <= 0) return SLIMDP_ERR_CUDA;
+    // more warps an output only while there are fewer than eight an SM and each has a stretch
+    uint32_t split = 0;
+    while (split < 3 && (warps << split) < 8ull * sms && (stretches >> (split + 1)) > 0) ++split;
+    const unsigned ctas = (unsigned)(((warps << split) + 7) / 8);
+    return with_rows(m, [&](auto rows) -> slimdp_status {
+        constexpr int M = decltype(rows)::value;
+        if (wide)
+            few_forward_kernel<T, kVec<T>, M><<<ctas, 256, 0, st>>>(x, ldx, w, ldw, (uint32_t)m, n, k, split, e);
+        else
+            few_forward_kernel<T, 1, M><<<ctas, 256, 0, st>>>(x, ldx, w, ldw, (uint32_t)m, n, k, split, e);
+        SLIMDP_LAUNCHED(1);
+        return SLIMDP_OK;
+    });
+}
+
+template slimdp_status launch_few_forward<float>(const float*, uint64_t, const float*, uint64_t, uint64_t, uint64_t, uint64_t,
+                                                 const Epilogue&, cudaStream_t);
+template slimdp_status launch_few_forward<__nv_bfloat16>(const __nv_bfloat16*, uint64_t, const __nv_bfloat16*, uint64_t,
+                                                         uint64_t, uint64_t, uint64_t, const Epilogue&, cudaStream_t);
+template slimdp_status launch_few_forward<__half>(const __half*, uint64_t, const __half*, uint64_t, uint64_t, uint64_t, uint64_t,
+                                                  const Epilogue&, cudaStream_t);
+
+}  // namespace slimdp

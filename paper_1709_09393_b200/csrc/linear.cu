@@ -10,99 +10,16 @@
 #include <atomic>
 #include <type_traits>
 
+#include "epilogue.cuh"
 #include "tensor.cuh"
-#include "train.cuh"
 
 namespace slimdp {
 
+template <typename T>
+slimdp_status launch_few_forward(const T* x, uint64_t ldx, const T* w, uint64_t ldw, uint64_t m, uint64_t n, uint64_t k,
+                                 const Epilogue& e, cudaStream_t st);
+
 namespace {
-
-// What is done with C[i, j] before it is stored; NULL members are left out.
-struct Epilogue {
-    const float* bias;                 // + bias[j]
-    void* z;  uint64_t ldz;            // pre-activation: written by forward, read by backward_input
-    const void* add;  uint64_t ldadd;  // residual or its gradient
-    void* out;  uint64_t ldo;
-    int act;
-    bool accumulate;                   // out is fp32 and keeps what it holds
-};
-
-enum Product { kForward, kInput, kWeight };
-
-// What the epilogue reads at V adjacent results: loaded for several places at once, before any of them is worked on.
-template <typename T, Product P, int V>
-struct Extra {
-    Pack<T, V> z, add;
-    Pack<float, V> old;
-
-    __device__ __forceinline__ void load(const Epilogue& e, uint64_t i, uint64_t j) {
-        if constexpr (P == kInput)
-            if (e.act != SLIMDP_ACT_NONE) z = load_pack<T, V>((const T*)e.z + i * e.ldz + j);
-        if constexpr (P == kWeight) {
-            if (e.accumulate) old = load_pack<float, V>((const float*)e.out + i * e.ldo + j);
-        } else {
-            if (e.add) add = load_pack<T, V>((const T*)e.add + i * e.ldadd + j);
-        }
-    }
-};
-
-// B times V adjacent results C[i + b step, j .. j + V) for b < count, through the epilogue of product P, one step of it for all of
-// them at a time; bias: the V values of these columns.
-template <typename T, Product P, int V, int B>
-__device__ __forceinline__ void finish(const Epilogue& e, uint64_t i, uint32_t step, uint32_t count, uint64_t j, float (&v)[B][V],
-                                       const float (&bias)[V], const Extra<T, P, V> (&x)[B]) {
-    if constexpr (P == kForward) {
-#pragma unroll
-        for (int b = 0; b < B; ++b)
-#pragma unroll
-            for (int c = 0; c < V; ++c) v[b][c] += bias[c];
-        if (e.z) {
-            T* const z = (T*)e.z + i * e.ldz + j;
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-                if (b < count) store_pack<T, V>(z + (uint64_t)(b * step) * e.ldz, v[b]);
-        }
-        with_act(e.act, [&](auto act) {
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-#pragma unroll
-                for (int c = 0; c < V; ++c) v[b][c] = act_value<decltype(act)::value>(v[b][c]);
-        });
-    } else if constexpr (P == kInput) {
-        with_act(e.act, [&](auto act) {
-#pragma unroll
-            for (int b = 0; b < B; ++b) {
-                float z[V];
-                unpack<T, V>(x[b].z, z);
-#pragma unroll
-                for (int c = 0; c < V; ++c) v[b][c] *= act_slope<decltype(act)::value>(z[c]);
-            }
-        });
-    }
-    if constexpr (P == kWeight) {
-        if (e.accumulate) {
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-#pragma unroll
-                for (int c = 0; c < V; ++c) v[b][c] += x[b].old.get(c);
-        }
-        float* const out = (float*)e.out + i * e.ldo + j;
-#pragma unroll
-        for (int b = 0; b < B; ++b)
-            if (b < count) store_pack<float, V>(out + (uint64_t)(b * step) * e.ldo, v[b]);
-    } else {
-        if (e.add) {
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-#pragma unroll
-                for (int c = 0; c < V; ++c) v[b][c] += x[b].add.get(c);
-        }
-        T* const out = (T*)e.out + i * e.ldo + j;
-#pragma unroll
-        for (int b = 0; b < B; ++b)
-            if (b < count) store_pack<T, V>(out + (uint64_t)(b * step) * e.ldo, v[b]);
-    }
-}
 
 // Elements of the type that product P stores that make 16 bytes.
 template <typename T, Product P>
@@ -850,6 +767,7 @@ slimdp_status launch_linear_forward(const void* x, uint64_t ldx, const void* w, 
     const Epilogue e = {bias, z, ldz, residual, ldr, y, ldy, act, false};
     return with_type(type, [&](auto v) {
         using T = decltype(v);
+        if (few_rows(m, n, k)) return launch_few_forward<T>((const T*)x, ldx, (const T*)w, ldw, m, n, k, e, st);
         return launch_product<T, kForward>({x, ldx, m, k}, {w, ldw, n, k}, m, n, k, e, Scratch{(uint8_t*)ws}, st);
     });
 }

@@ -417,6 +417,24 @@ def test_distill(P, dtype, rows, vocab, top):
     distill_check(P, logits, idx, teacher.to(torch.float16), label, weight, 1.0, 0.5, 0.5)
 
 
+@pytest.mark.parametrize("rows,vocab,top,dtype", [(6000, 500, 6, torch.float32), (2500, 9000, 40, torch.bfloat16),
+                                                  (700, 30001, 64, torch.float16), (260, 131072, 64, torch.bfloat16),
+                                                  (150, 131072, 300, torch.float32), (90, 200000, 64, torch.bfloat16)])
+def test_distill_of_many_more_rows_than_run_at_once(P, rows, vocab, top, dtype):
+    """Rows follow one another through the same buffers; some have no term, so that neighbours are of different lengths."""
+    g = gen(rows)
+    logits = matrix(rows, vocab, dtype, g, 3.0)
+    idx = torch.randint(0, vocab, (rows, top), generator=g, device="cuda").to(torch.int32)
+    idx[::7] = -1
+    teacher = torch.randn(rows, top, generator=g, device="cuda") * 2
+    label = torch.randint(0, vocab, (rows,), generator=g, device="cuda").to(torch.int32)
+    weight = torch.rand(rows, generator=g, device="cuda")
+    weight[::5] = 0
+    distill_check(P, logits, idx, teacher, None, weight, 2.0, 1.0, 0.0)
+    distill_check(P, logits, idx, teacher, label, weight, 2.0, 0.5, 0.5)
+    distill_check(P, logits, idx, teacher, label, weight, 3.0, 0.5, 0.5)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("pad,offset", [(8, 0), (0, 8), (3, 0), (0, 1), (5, 3)])
 def test_distill_rows_of_any_alignment(P, dtype, pad, offset):

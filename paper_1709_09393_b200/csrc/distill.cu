@@ -766,6 +766,235 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
     cluster_sync();
 }
 
+// Rows of up to 32 PIECES pieces: a warp each, its exponentials in registers, everything between its own lanes.  Sixteen such warps an SM
+// hide each other's latency without any of the slices' machinery, whose four kinds of warps meet several times a row.
+constexpr int kRowWarps = 4;
+
+template <typename T, int PIECES, int SECOND>
+__global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T* logits, T* dlogits, const DistillArgs a) {
+    constexpr int V = kVec<T>;
+    extern __shared__ int32_t entries[];
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slots = table_slots(a.top), table_shift = 32 - (__ffs(slots) - 1);
+    int32_t* const s_idx = entries + warp * (4 * a.top + slots);
+    float* const s_t = reinterpret_cast<float*>(s_idx + a.top);
+    float *const s_q = s_t + a.top, *const s_z = s_q + a.top;
+    int32_t* const table = reinterpret_cast<int32_t*>(s_z + a.top);
+    const uint32_t top = a.kd != 0.0f ? a.top : 0u;
+    const float c_t = kLog2e / a.temperature, c_1 = kLog2e, c = a.kd != 0.0f ? c_t : c_1;
+    for (uint32_t s = lane; s < slots; s += 32) table[s] = -1;
+    __syncwarp();
+    for (uint64_t row = (uint64_t)blockIdx.x * kRowWarps + warp; row < a.rows; row += (uint64_t)gridDim.x * kRowWarps) {
+        const T* const z = logits + row * a.ldl;
+        T* const out = dlogits ? dlogits + row * a.ldd : nullptr;
+        const Part p = part_of(z, a.vocab, 0, 0);
+        const uint32_t tail = p.head + p.pieces * V;
+        const bool head_mine = lane < p.head, tail_mine = lane < a.vocab - tail;
+        alignas(16) uint32_t raw[PIECES][4], most = Words<T>::lowest;
+        float single[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            uint4 q = make_uint4(Words<T>::lowest, Words<T>::lowest, Words<T>::lowest, Words<T>::lowest);
+            if (i * 32 + lane < p.pieces) q = *reinterpret_cast<const uint4*>(z + p.head + (i * 32 + lane) * V);
+            raw[i][0] = q.x, raw[i][1] = q.y, raw[i][2] = q.z, raw[i][3] = q.w;
+        }
+        if (head_mine) single[0] = to_f32(z[lane]);
+        if (tail_mine) single[1] = to_f32(z[tail + lane]);
+        // the teacher's entries, and the logits there
+        const float w = a.weight ? __ldg(a.weight + row) : 1.0f;
+        const int32_t y = a.label ? __ldg(a.label + row) : -1;
+        const bool has_label = a.ce != 0.0f && y >= 0 && (uint32_t)y < a.vocab;
+        const float z_label = has_label ? to_f32(z[y]) : 0.0f;
+        float tmax = -INFINITY, total = 0.0f;
+        bool any = false;
+        for (uint32_t j = lane; j < top; j += 32) {
+            const int32_t i = a.idx[row * a.top + j];
+            const bool there = i >= 0 && (uint32_t)i < a.vocab;
+            const float t = there ? load_teacher(a.teacher, a.teacher_type, row * a.top + j) : -INFINITY;
+            s_idx[j] = there ? i : -1;
+            s_t[j] = t;
+            s_z[j] = there ? to_f32(z[i]) : 0.0f;
+            tmax = fmaxf(tmax, t);
+            any |= t != -INFINITY;
+        }
+        const bool has_teacher = __any_sync(0xFFFFFFFFu, any);
+        tmax = warp_max(tmax);
+        for (uint32_t j = lane; j < top; j += 32) total += s_q[j] = exp2_approx((s_t[j] - tmax) * c_t);
+        total = warp_sum(total);
+        const float coef_t = has_teacher ? w * a.kd * a.temperature : 0.0f, coef_1 = has_label ? w * a.ce : 0.0f;
+
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) most = Words<T>::max(most, raw[i][u]);
+        const float m_row = warp_max(fmaxf(Words<T>::top(most), fmaxf(single[0], single[1])));
+        const float m = m_row == -INFINITY ? 0.0f : m_row, off = fabsf(m) < kFar ? 0.0f : m;   // taken away first where m c does not fit
+        const float k = reference(m, c), k_1 = reference_1<SECOND>(m, c, c_1);
+        const uint64_t by2 = pair_of(c, c), k2 = pair_of(-k, -k), by2_1 = pair_of(c_1, c_1), k2_1 = pair_of(-k_1, -k_1);
+        const uint64_t less = pair_of(-off, -off);
+        uint64_t e[PIECES * V / 2], sum2 = pair_of(0.0f, 0.0f), other2 = sum2;
+        auto logit = [&](int i, int u) {
+            const uint64_t x = Words<T>::pair(raw[i], u);
+            return off != 0.0f ? add_pair(x, less) : x;
+        };
+        // the second exponential of a pair of logits s whose first is x
+        auto second = [&](uint64_t s, uint64_t x) {
+            if constexpr (SECOND == kOwnSecond) {
+                float lo, hi;
+                split_pair(fma_pair(s, by2_1, k2_1), lo, hi);
+                return pair_of(exp2_approx(lo), exp2_approx(hi));
+            } else {
+                return power<SECOND>(x);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int u = 0; u < V / 2; ++u) {
+                float lo, hi;
+                split_pair(fma_pair(logit(i, u), by2, k2), lo, hi);
+                const uint64_t x = pair_of(exp2_approx(lo), exp2_approx(hi));
+                e[i * (V / 2) + u] = x;
+                sum2 = add_pair(sum2, x);
+                if constexpr (SECOND != kNoSecond) other2 = add_pair(other2, second(logit(i, u), x));
+            }
+        auto second_of = [&](float v, float x) {
+            if (SECOND == kNoSecond) return 0.0f;
+            return SECOND == kOwnSecond ? exp2_approx(fmaf(v - off, c_1, -k_1)) : power<SECOND>(x);
+        };
+        float sum_t, sum_1, lo, hi, single_1[2] = {};
+        split_pair(sum2, lo, hi);
+        sum_t = lo + hi;
+        split_pair(other2, lo, hi);
+        sum_1 = lo + hi;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float v = single[i];
+            single[i] = exp2_approx(fmaf(v - off, c, -k));
+            single_1[i] = second_of(v, single[i]);
+            sum_t += single[i], sum_1 += single_1[i];
+        }
+        sum_t = warp_sum(sum_t);
+        sum_1 = SECOND != kNoSecond ? warp_sum(sum_1) : sum_t;
+        // a row without a term, or with nothing but -inf, has gradient 0, whatever it holds
+        const bool none = sum_t == 0.0f || (coef_t == 0.0f && coef_1 == 0.0f);
+
+        float sum_q = 0.0f, term = 0.0f;
+        bool shared = false;
+        if (coef_t != 0.0f) {
+            for (uint32_t j = lane; j < top; j += 32)
+                if (s_idx[j] >= 0 && s_q[j] != 0.0f) {
+                    sum_q += s_q[j];
+                    term += s_q[j] * ((s_t[j] - tmax) - (s_z[j] - m));
+                }
+            sum_q = warp_sum(sum_q) / total, term = warp_sum(term) / total;
+        }
+        float loss = 0.0f;
+        // T (log q - log p^T) with the temperature multiplied out: (s - m) / T would overflow for the lowest values that masks
+        // put in place of logits
+        if (coef_t != 0.0f) loss = a.kd * a.temperature * (term + sum_q * a.temperature * (log_sum(sum_t, m, c) - logf(total)));
+        if (has_label)
+            loss += a.ce * (log_sum(sum_1, m, SECOND == kOwnSecond ? c_1 : c, SECOND > kOwnSecond ? SECOND : 1) - (z_label - m));
+        if (lane == 0) a.loss[row] = none ? 0.0f : w * loss;
+        if (!out) continue;
+
+        const float g = none ? 0.0f : (SECOND ? coef_t : coef_t + coef_1) / sum_t, g_1 = SECOND && !none ? coef_1 / sum_1 : 0.0f;
+        const uint64_t g2 = pair_of(g, g), g2_1 = pair_of(g_1, g_1);
+        const bool wide = (reinterpret_cast<uintptr_t>(out + p.head) & 15u) == 0;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            if (i * 32 + lane < p.pieces) {
+                float v[V];
+                uint64_t s[V / 2] = {};
+                if constexpr (SECOND == kOwnSecond) {     // the logits are read again: registers hold their exponentials
+                    unpack<T, V>(load_pack<T, V>(z + p.head + (i * 32 + lane) * V), v);
+#pragma unroll
+                    for (int u = 0; u < V / 2; ++u) s[u] = add_pair(pair_of(v[2 * u], v[2 * u + 1]), less);
+                }
+#pragma unroll
+                for (int u = 0; u < V / 2; ++u) {
+                    uint64_t x = e[i * (V / 2) + u];
+                    // its power is computed again: the first one would be kept in as many registers as e
+                    if constexpr (SECOND != kNoSecond) asm volatile("" : "+l"(x));
+                    uint64_t r = mul_pair(g2, x);
+                    if constexpr (SECOND != kNoSecond) r = fma_pair(g2_1, second(s[u], x), r);
+                    split_pair(r, v[2 * u], v[2 * u + 1]);
+                }
+                if (none)
+#pragma unroll
+                    for (int u = 0; u < V; ++u) v[u] = 0.0f;
+                T* const o = out + p.head + (i * 32 + lane) * V;
+                if (wide) {
+                    store_pack<T, V>(o, v);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < V; ++u) o[u] = from_f32<T>(v[u]);
+                }
+            }
+        if (head_mine) out[lane] = from_f32<T>(none ? 0.0f : g * single[0] + g_1 * single_1[0]);
+        if (tail_mine) out[tail + lane] = from_f32<T>(none ? 0.0f : g * single[1] + g_1 * single_1[1]);
+        // entries that share an index: found by putting the indices into a table, and only then told apart
+        if (!none && coef_t != 0.0f) {
+            for (uint32_t j = lane; j < top; j += 32) {
+                const int32_t i = s_idx[j];
+                if (i < 0) continue;
+                uint32_t s = ((uint32_t)i * 2654435761u) >> table_shift;
+                int32_t was;
+                while ((was = atomicCAS(table + s, -1, i)) != -1 && was != i) s = (s + 1) & (slots - 1);
+                shared |= was == i;
+                s_t[j] = __uint_as_float(s);              // the teacher's logits are not needed any more
+            }
+            shared = __any_sync(0xFFFFFFFFu, shared);
+        }
+        __syncwarp();            // the dense result is stored; the entries go over it
+        if (!none) {
+            auto dense = [&](float v) {
+                const float x = exp2_approx(fmaf(v - off, c, -k));
+                return fmaf(g_1, second_of(v, x), g * x);
+            };
+            bool taken = false;  // the label is also an entry of the teacher
+            if (coef_t != 0.0f)
+                for (uint32_t j = lane; j < top; j += 32) {
+                    const int32_t i = s_idx[j];
+                    if (i < 0) continue;
+                    table[__float_as_uint(s_t[j])] = -1;
+                    taken |= has_label && i == y;
+                    float q = s_q[j];
+                    bool leads = true;
+                    if (shared) {                         // the first of them stands for the sum
+                        q = 0.0f;
+                        for (uint32_t l = 0; l < top; ++l)
+                            if (s_idx[l] == i) {
+                                q += s_q[l];
+                                leads = leads && l >= j;
+                            }
+                    }
+                    if (leads) out[i] = from_f32<T>(dense(s_z[j]) - coef_t * (q / total) - (has_label && i == y ? coef_1 : 0.0f));
+                }
+            taken = __any_sync(0xFFFFFFFFu, taken);
+            if (lane == 0 && has_label && !taken) out[y] = from_f32<T>(dense(z_label) - coef_1);
+        }
+        __syncwarp();
+    }
+}
+
+template <typename T, int PIECES, int SECOND>
+slimdp_status launch_rows(const T* logits, T* dlogits, const DistillArgs& a, cudaStream_t st) {
+    static DeviceOnce once;
+    auto kernel = distill_row_kernel<T, PIECES, SECOND>;
+    auto smem = [](uint32_t top) { return kRowWarps * (4 * top + table_slots(top)) * 4; };
+    if (once.needed()) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem(SLIMDP_MAX_TOP)) != cudaSuccess)
+            return SLIMDP_ERR_CUDA;
+        once.mark();
+    }
+    const int sms = sm_count();
+    if (sms <= 0) return SLIMDP_ERR_CUDA;
+    const unsigned ctas = (unsigned)std::min<uint64_t>((a.rows + kRowWarps - 1) / kRowWarps, (uint64_t)sms * 4);
+    kernel<<<ctas, 32 * kRowWarps, smem(a.top), st>>>(logits, dlogits, a);
+    SLIMDP_LAUNCHED(1);
+    return SLIMDP_OK;
+}
+
 template <typename T, int WARPS, int PIECES, int CTAS, int SECOND>
 slimdp_status launch_slices(const T* logits, T* dlogits, const DistillArgs& a, uint32_t ranks, cudaStream_t st) {
     using S = SliceShape<T, WARPS, PIECES>;
@@ -806,7 +1035,8 @@ slimdp_status launch_slices(const T* logits, T* dlogits, const DistillArgs& a, u
 
 template <typename T, int SECOND>
 slimdp_status launch_by_length(const T* z, T* d, const DistillArgs& a, uint64_t pieces, cudaStream_t st) {
-    if (pieces <= 256) return launch_slices<T, 2, 4, 8, SECOND>(z, d, a, 1, st);
+    if (pieces <= 32 * 2) return launch_rows<T, 2, SECOND>(z, d, a, st);
+    if (pieces <= 32 * 8) return launch_rows<T, 8, SECOND>(z, d, a, st);
     for (uint32_t ranks = 1; ranks <= 8; ranks *= 2)
         if (pieces <= (uint64_t)ranks * 2048) return launch_slices<T, 8, 8, 2, SECOND>(z, d, a, ranks, st);
     return launch_slices<T, 16, 8, 1, SECOND>(z, d, a, 8, st);

@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(256) pack_kernel(PackJob job0, PackJob job1) {
     }
 }
 
-uint64_t packed_ld(uint64_t cols) { return align_up(cols, 8); }
+uint64_t packed_ld(uint64_t cols) { return align_up(cols, 64); }     // rows on 128-byte boundaries
 size_t packed_bytes(uint64_t rows, uint64_t cols, int32_t type) {
     return align_up(rows * packed_ld(cols) * 2 * (type == SLIMDP_F32 ? 3 : 1), 256);
 }
@@ -667,25 +667,31 @@ struct Plan {
 
 uint64_t partial_bytes(uint64_t m, uint64_t n) { return m * align_up(n, 8) * 4; }
 
-// The cut with the least estimated time, in ns, from what was measured on one B200.  A stage of 64 summed indices takes a CTA as long
-// as its products (2 cycles a column at 1.9 GHz) or as its bytes at 110 a ns, the rate at which L2 feeds an SM while all
-// ask, and 180 at least; a tile's epilogue that nothing follows 600 and 350 more for each 64 columns.  A split adds a second kernel that reads
-// the partial sums (2500, and 5000 bytes a ns).  Large products end with 256 x 256, whose stage is bound by its products.
-Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts) {
+// The cut with the least estimated time, in ns, from what was measured on one B200 (bf16, all SMs busy).  `stage`: 64 summed indices
+// of a tile; the narrow tiles are bound by what the tensor cores read from shared memory and by L2, whose part doubles where
+// rows of an operand are not on 128-byte boundaries, 256 x 256 by its products.  `fixed`: from the launch to the first stage and from the
+// last to the end, most of it the epilogue of the last tile; `finish`: an epilogue that the next tile's products cover, or wait for.  A
+// split adds a second kernel that reads the partial sums.
+struct Shape {
+    uint32_t pair, width;
+    double stage, fixed, finish;
+};
+constexpr Shape kShapes[] = {{2, 256, 340, 8300, 4400}, {2, 128, 180, 6500, 2200}, {1, 128, 195, 4900, 2200}, {1, 64, 165, 3800, 1100}};
+
+Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts, bool lines) {
     const uint64_t sms = 148;
     Plan best = {};
     double least = 0.0;
-    for (const Plan shape : {Plan{2, 256, 1}, Plan{2, 128, 1}, Plan{1, 128, 1}, Plan{1, 64, 1}}) {
+    for (const Shape& shape : kShapes) {
         const uint64_t tiles = ((m + 128 * shape.pair - 1) / (128 * shape.pair)) * ((n + shape.width - 1) / shape.width);
         const uint64_t slots = sms / shape.pair;
-        const double bytes = 128.0 * (std::min<uint64_t>(m, 128) + std::min<uint64_t>(n, shape.width / shape.pair));
-        const double stage = std::max({2.0 * shape.width / 1.9, bytes / 110.0, 180.0});
+        const double stage = lines || shape.width == 256 ? shape.stage : 2.0 * shape.stage;
         uint64_t most = tiles * 2 <= slots ? std::min(slots / tiles, std::max<uint64_t>(kblocks / 4, 1)) : 1;
         most = std::max<uint64_t>(1, std::min(most, kPartialBytes / partial_bytes(m, n)));
-        for (uint64_t splits : {uint64_t(1), most}) {
+        for (uint64_t splits : {uint64_t(1), std::min<uint64_t>(most, 2), std::min<uint64_t>(most, 4), most}) {
             const double waves = (double)((tiles * splits + slots - 1) / slots), steps = (double)((kblocks + splits - 1) / splits * parts);
-            double t = waves * steps * stage + 600.0 + 350.0 * shape.width / 64;
-            if (splits > 1) t += 2500.0 + (double)(splits * partial_bytes(m, n)) / 5000.0;
+            double t = shape.fixed + std::max(waves * steps * stage, steps * stage + (waves - 1) * shape.finish);
+            if (splits > 1) t += 2200.0 + (double)(splits * partial_bytes(m, n)) / 3700.0;
             if (best.pair == 0 || t < least) {
                 least = t;
                 best = {shape.pair, shape.width, (uint32_t)splits};
@@ -713,7 +719,8 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
     const uint64_t size = P == kWeight ? 4 : sizeof(T);
     auto starts_wide = [&](const void* p, uint64_t ld) { return !p || (aligned16(p) && (ld * size) % 16 == 0); };
     args.wide = starts_wide(e.out, e.ldo) && starts_wide(e.z, e.ldz) && starts_wide(e.add, e.ldadd);
-    const Plan plan = plan_product(m, n, args.kblocks, kParts == 3 ? 6 : 1);
+    const bool lines = a.ld % 64 == 0 && b.ld % 64 == 0;      // rows of both operands on 128-byte boundaries
+    const Plan plan = plan_product(m, n, args.kblocks, kParts == 3 ? 6 : 1, lines);
     args.splits = plan.splits;
     args.tiles_m = (uint32_t)((m + 128 * plan.pair - 1) / (128 * plan.pair));
     args.tiles_n = (uint32_t)((n + plan.width - 1) / plan.width);
@@ -748,8 +755,12 @@ size_t linear_ws_bytes(uint64_t m, uint64_t n, uint64_t k, int32_t type) {
     const uint64_t x = packed_bytes(m, k, type), w = packed_bytes(n, k, type), dy = packed_bytes(m, n, type);
     auto partial = [&](uint64_t rows, uint64_t cols, uint64_t summed) -> uint64_t {
         if (rows == 0 || summed == 0) return 0;
-        const Plan p = plan_product(rows, cols, (summed + kBk - 1) / kBk, type == SLIMDP_F32 ? 6 : 1);
-        return p.splits > 1 ? align_up(p.splits * partial_bytes(rows, cols), 256) : 0;
+        uint64_t most = 0;       // whichever way the rows lie
+        for (bool lines : {false, true}) {
+            const Plan p = plan_product(rows, cols, (summed + kBk - 1) / kBk, type == SLIMDP_F32 ? 6 : 1, lines);
+            if (p.splits > 1) most = std::max(most, align_up(p.splits * partial_bytes(rows, cols), 256));
+        }
+        return most;
     };
     return 256 + std::max({x + w + partial(m, n, k), dy + w + partial(m, k, n), dy + x + partial(n, k, m)});
 }

@@ -33,7 +33,18 @@ constexpr int kProductThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
 // Registers of a chunked product's warps: its sums take 128 of an epilogue warp.  The kernel starts with 168 for each of its twelve
 // warps, and 4 x 56 + 8 x 224 = 12 x 168.
 constexpr int kLoaderRegs = 56, kEpilogueRegs = 224;
-constexpr int kEpiloguePitch = 33;           // floats of a row of a warp's 32 x 32 staging square
+
+// Place of (row, column) in a warp's 32 x 32 staging square: 16-byte chunks of a row are permuted by the row, so that a lane can write
+// its row and read its columns 16 bytes at a time without two lanes meeting in a bank.
+__device__ __forceinline__ uint32_t square_place(uint32_t row, uint32_t column) {
+    return row * 32 + (((column >> 2) ^ (row & 7u)) << 2) + (column & 3u);
+}
+
+__device__ __forceinline__ void write_square(float* square, uint32_t lane, const float (&v)[32]) {
+#pragma unroll
+    for (int c = 0; c < 32; c += 4)
+        *reinterpret_cast<float4*>(square + square_place(lane, c)) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+}
 
 // A wait in a product kernel ran out on this device (never, unless the device misbehaves).
 __device__ int g_product_status;
@@ -87,9 +98,18 @@ __device__ __forceinline__ void finish_square_by(const ProductArgs& args, uint32
         }
         float v[B][V];
 #pragma unroll
-        for (int b = 0; b < B; ++b)
+        for (int b = 0; b < B; ++b) {
+            const uint32_t k = min(k0 + b * V, 31u);
+            if constexpr (V == 1) {
+                v[b][0] = square[square_place(k, c)];
+            } else {
 #pragma unroll
-            for (int u = 0; u < V; ++u) v[b][u] = square[min(k0 + b * V, 31u) * kEpiloguePitch + c + u];
+                for (int u = 0; u < V; u += 4) {
+                    const float4 q = *reinterpret_cast<const float4*>(square + square_place(k, c + u));
+                    v[b][u] = q.x, v[b][u + 1] = q.y, v[b][u + 2] = q.z, v[b][u + 3] = q.w;
+                }
+            }
+        }
         if constexpr (PARTIAL) {
             float* const out = args.partial + ((uint64_t)split * args.m + i) * args.ld_partial + j;
 #pragma unroll
@@ -119,7 +139,7 @@ __device__ __forceinline__ void finish_square(const ProductArgs& args, uint32_t 
 template <int CG, int BN>
 struct ProductShape {
     static constexpr uint32_t a_bytes = 128 * kBk * 2, b_bytes = BN / CG * kBk * 2, stage = a_bytes + b_bytes;
-    static constexpr uint32_t epilogue = kEpilogueWarps * 32 * kEpiloguePitch * 4, control = 512;
+    static constexpr uint32_t epilogue = kEpilogueWarps * 32 * 32 * 4, control = 512;
     static constexpr uint32_t stages = (232448 - 1024 - epilogue - control) / stage < 8 ? (232448 - 1024 - epilogue - control) / stage : 8;
     static constexpr uint32_t smem = stages * stage + epilogue + control + 1024;
     static constexpr uint32_t columns = 2 * BN;     // two accumulators
@@ -265,7 +285,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     } else {
         if constexpr (kChunked<T, P>) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
         const uint32_t quarter = warp & 3u, half = (warp - kFirstEpilogueWarp) >> 2;
-        float* const square = reinterpret_cast<float*>(smem + S::stages * S::stage) + (warp - kFirstEpilogueWarp) * 32 * kEpiloguePitch;
+        float* const square = reinterpret_cast<float*>(smem + S::stages * S::stage) + (warp - kFirstEpilogueWarp) * 32 * 32;
         constexpr int kSquares = BN / 64;             // of 32 x 32 results of this warp
         const uint32_t lanes = tmem + ((quarter * 32) << 16) + half * (BN / 2);
         uint32_t count = 0;
@@ -297,10 +317,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 for (int q = 0; q < kSquares; ++q) {
 #pragma unroll
                     for (int u = 0; u < kSquares; ++u)
-                        if (u == q) {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) square[lane * kEpiloguePitch + c] = sum[u][c];
-                        }
+                        if (u == q) write_square(square, lane, sum[u]);
                     __syncwarp();
                     finish_square<T, P>(args, split, square, row0, col0 + q * 32, lane);
                     __syncwarp();
@@ -314,8 +331,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     {
                         float v[32];
                         tmem_load32(lanes + buf * BN + q * 32, v);
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) square[lane * kEpiloguePitch + c] = v[c];
+                        write_square(square, lane, v);
                     }
                     if (q == kSquares - 1) tc_fence_before();      // the accumulator has been read
                     __syncwarp();
@@ -515,7 +531,7 @@ struct PackJob {
     const void* src;
     void* dst;
     uint64_t ld, ld_dst, rows, cols;
-    bool wide;
+    uint32_t grain;      // rows start on multiples of this many bytes
 };
 
 template <typename T>
@@ -528,7 +544,7 @@ __global__ void __launch_bounds__(256) pack_kernel(PackJob job0, PackJob job1) {
         // ld_dst is a multiple of eight: whole groups fit
         if constexpr (sizeof(T) == 4) {
             float v[8], part[8][3];
-            if (job.wide && j + 8 <= job.cols) {
+            if (job.grain == 16 && j + 8 <= job.cols) {
                 unpack<T, 4>(load_pack<T, 4>(src), v);
                 unpack<T, 4>(load_pack<T, 4>(src + 4), v + 4);
             } else {
@@ -545,13 +561,22 @@ __global__ void __launch_bounds__(256) pack_kernel(PackJob job0, PackJob job1) {
                 store_pack<__nv_bfloat16, 8>((__nv_bfloat16*)job.dst + ((uint64_t)p * job.rows + i) * job.ld_dst + j, f);
             }
         } else {
-            // 16-bit operands come here only where their rows are not on 16-byte boundaries; values move as they are
+            // 16-bit operands come here only where their rows are not on 16-byte boundaries; values move as they are, in the largest
+            // pieces that the rows allow
             const uint16_t* const bits = (const uint16_t*)src;
             uint32_t w[4];
+            if (job.grain == 8 && j + 8 <= job.cols) {
+                const uint2 lo = reinterpret_cast<const uint2*>(bits)[0], hi = reinterpret_cast<const uint2*>(bits)[1];
+                w[0] = lo.x, w[1] = lo.y, w[2] = hi.x, w[3] = hi.y;
+            } else if (job.grain >= 4 && j + 8 <= job.cols) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const uint32_t lo = j + 2 * u < job.cols ? bits[2 * u] : 0u, hi = j + 2 * u + 1 < job.cols ? bits[2 * u + 1] : 0u;
-                w[u] = lo | hi << 16;
+                for (int u = 0; u < 4; ++u) w[u] = reinterpret_cast<const uint32_t*>(bits)[u];
+            } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t lo = j + 2 * u < job.cols ? bits[2 * u] : 0u, hi = j + 2 * u + 1 < job.cols ? bits[2 * u + 1] : 0u;
+                    w[u] = lo | hi << 16;
+                }
             }
             *reinterpret_cast<uint4*>((T*)job.dst + i * job.ld_dst + j) = make_uint4(w[0], w[1], w[2], w[3]);
         }
@@ -613,7 +638,8 @@ slimdp_status prepare_operands(Matrix& a, Matrix& b, Scratch& ws, cudaStream_t s
         if (!kSplit && wide) continue;
         const uint64_t ld = packed_ld(x->cols);
         void* dst = ws.take(packed_bytes(x->rows, x->cols, kSplit ? SLIMDP_F32 : SLIMDP_BF16));
-        job[jobs++] = {x->p, dst, x->ld, ld, x->rows, x->cols, wide};
+        const uint64_t at = reinterpret_cast<uintptr_t>(x->p) | (x->ld * sizeof(T)) | 16;
+        job[jobs++] = {x->p, dst, x->ld, ld, x->rows, x->cols, (uint32_t)(at & (~at + 1))};
         most = std::max(most, x->rows * (ld / 8));
         x->p = dst;
         x->ld = ld;

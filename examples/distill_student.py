@@ -1,0 +1,178 @@
+"""Slim-DP training of a small residual student from a teacher's top logits, every step on the device.
+
+K workers hold a local copy of the flat fp32 model each.  A worker's local step runs the library's operators on
+slices of that vector: layer norm, two matrix products with activation and residual in their epilogues, a projection to the
+vocabulary and the distillation loss; backward, every parameter gradient lands in the matching slice of the worker's flat
+update.  The updates then go through the communication rounds of SlimDPDriver: dense pushes every q-th round, the
+communication set in between.
+
+    python examples/distill_student.py --rounds 40 --dtype bf16
+"""
+from __future__ import annotations
+
+import argparse
+import math
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_1709_09393_b200 as P  # noqa: E402
+
+EPS = 1e-5
+
+
+class Layout:
+    """Names and places of the parameters in the flat vector."""
+
+    def __init__(self, blocks: int, dim: int, hidden: int, vocab: int):
+        self.blocks, self.dim, self.hidden, self.vocab = blocks, dim, hidden, vocab
+        self.at, self.n = {}, 0
+        for b in range(blocks):
+            for name, shape in (("gamma", (dim,)), ("beta", (dim,)), ("w1", (hidden, dim)), ("b1", (hidden,)),
+                                ("w2", (dim, hidden)), ("b2", (dim,))):
+                self._add(f"{b}.{name}", shape)
+        for name, shape in (("gamma", (dim,)), ("beta", (dim,)), ("wv", (vocab, dim)), ("bv", (vocab,))):
+            self._add(name, shape)
+
+    def _add(self, name, shape):
+        self.at[name] = (self.n, shape)
+        self.n += math.prod(shape)
+
+    def view(self, flat: torch.Tensor, name: str) -> torch.Tensor:
+        start, shape = self.at[name]
+        return flat[start:start + math.prod(shape)].view(shape)
+
+    def init(self, seed: int) -> torch.Tensor:
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        flat = torch.zeros(self.n, device="cuda")
+        for name, (_, shape) in self.at.items():
+            if len(shape) == 2:
+                self.view(flat, name).copy_(torch.randn(shape, generator=g, device="cuda") / math.sqrt(shape[1]))
+            elif name.endswith("gamma"):
+                self.view(flat, name).fill_(1.0)
+        return flat
+
+
+class Worker:
+    """The buffers of a worker's local step and the calls it makes, for batches of `tokens` rows."""
+
+    def __init__(self, lay: Layout, tokens: int, dtype: torch.dtype, top: int):
+        self.lay, self.tokens, self.dtype = lay, tokens, dtype
+
+        def new(rows, cols, t=dtype):
+            return torch.empty(rows, cols, device="cuda", dtype=t)
+
+        m, d, h, v = tokens, lay.dim, lay.hidden, lay.vocab
+        self.x = [new(m, d) for _ in range(lay.blocks + 1)]          # the residual stream
+        self.norm = [new(m, d) for _ in range(lay.blocks + 1)]
+        self.stats = [torch.empty(2, m, device="cuda") for _ in range(lay.blocks + 1)]
+        self.z = [new(m, h) for _ in range(lay.blocks)]              # pre-activations
+        self.a = [new(m, h) for _ in range(lay.blocks)]
+        self.logits = new(m, v)
+        self.loss = torch.empty(m, device="cuda")
+        self.dx, self.dnorm, self.dz, self.dres = new(m, d), new(m, d), new(m, h), new(m, d)
+        self.row_weight = torch.full((m,), 1.0 / m, device="cuda")
+        size = max(P.layernorm_workspace_bytes(m, d), P.linear_workspace_bytes(m, h, d, dtype),
+                   P.linear_workspace_bytes(m, d, h, dtype), P.linear_workspace_bytes(m, v, d, dtype))
+        self.ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def step(self, flat, delta, batch, teacher_idx, teacher_logit, label, temperature=2.0, kd=0.9, ce=0.1):
+        """Mean loss of a batch; its gradient is added to delta.  flat and delta: [n] fp32."""
+        lay, ws = self.lay, self.ws
+        p = lambda name: lay.view(flat, name)                                     # noqa: E731
+        g = lambda name: lay.view(delta, name)                                    # noqa: E731
+        # the products want the weights in their own type: fp32 slices as they are, else a copy for this step
+        weight = {n: p(n).to(self.dtype) for n, (_, s) in lay.at.items() if len(s) == 2}
+
+        self.x[0].copy_(batch)
+        for b in range(lay.blocks):
+            mean, rstd = self.stats[b]
+            P.slimdp_layernorm_forward(self.x[b], p(f"{b}.gamma"), p(f"{b}.beta"), EPS, self.norm[b], mean, rstd)
+            P.slimdp_linear_forward(self.norm[b], weight[f"{b}.w1"], p(f"{b}.b1"), self.a[b], ws, activation="gelu", z=self.z[b])
+            P.slimdp_linear_forward(self.a[b], weight[f"{b}.w2"], p(f"{b}.b2"), self.x[b + 1], ws, residual=self.x[b])
+        mean, rstd = self.stats[-1]
+        P.slimdp_layernorm_forward(self.x[-1], p("gamma"), p("beta"), EPS, self.norm[-1], mean, rstd)
+        P.slimdp_linear_forward(self.norm[-1], weight["wv"], p("bv"), self.logits, ws)
+        # the gradient takes the logits' place
+        P.slimdp_distill(self.logits, teacher_idx, teacher_logit, self.loss, self.logits, label=label,
+                         row_weight=self.row_weight, temperature=temperature, kd_weight=kd, ce_weight=ce)
+
+        P.slimdp_linear_backward_weight(self.logits, self.norm[-1], g("wv"), g("bv"), ws, accumulate=True)
+        P.slimdp_linear_backward_input(self.logits, weight["wv"], self.dnorm, ws)
+        P.slimdp_layernorm_backward(self.dnorm, self.x[-1], p("gamma"), mean, rstd, self.dx, g("gamma"), g("beta"), ws,
+                                    accumulate=True)
+        for b in reversed(range(lay.blocks)):
+            # dx is the gradient of x[b + 1] = x[b] + a w2^T + b2
+            P.slimdp_linear_backward_weight(self.dx, self.a[b], g(f"{b}.w2"), g(f"{b}.b2"), ws, accumulate=True)
+            P.slimdp_linear_backward_input(self.dx, weight[f"{b}.w2"], self.dz, ws, activation="gelu", z=self.z[b])
+            P.slimdp_linear_backward_weight(self.dz, self.norm[b], g(f"{b}.w1"), g(f"{b}.b1"), ws, accumulate=True)
+            P.slimdp_linear_backward_input(self.dz, weight[f"{b}.w1"], self.dnorm, ws)
+            mean, rstd = self.stats[b]
+            P.slimdp_layernorm_backward(self.dnorm, self.x[b], p(f"{b}.gamma"), mean, rstd, self.dres, g(f"{b}.gamma"),
+                                        g(f"{b}.beta"), ws, accumulate=True)
+            self.dx += self.dres
+        return self.loss
+
+
+def synthetic_teacher(lay: Layout, seed: int, top: int):
+    """A fixed map from inputs to the top logits of a 'teacher': what a larger model would have written down."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    net = torch.randn(lay.dim, lay.vocab, generator=g, device="cuda") * (3.0 / math.sqrt(lay.dim))
+
+    def teach(x):
+        logit, idx = torch.topk(torch.tanh(x) @ net, top, dim=1)
+        return idx.to(torch.int32).contiguous(), logit.contiguous(), idx[:, 0].to(torch.int32).contiguous()
+
+    return teach
+
+
+def train(rounds=40, workers=4, blocks=2, dim=64, hidden=256, vocab=200, tokens=1024, top=16, dtype=torch.bfloat16,
+          lr=3.0, local_steps=2, q=8, core=0.10, explore=0.05, seed=0):
+    """Mean loss of each round; prints nothing."""
+    lay = Layout(blocks, dim, hidden, vocab)
+    w0 = lay.init(seed)
+    k_core = int(lay.n * core)
+    driver = P.SlimDPDriver(w0, workers, k_core, int((lay.n - k_core) * explore), q, c=1.0, eta=1.0 / workers, seed=seed)
+    worker = Worker(lay, tokens, dtype, top)                    # one device: the workers take turns with the buffers
+    teach = synthetic_teacher(lay, seed + 1, top)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed + 2)
+    deltas = [torch.zeros(lay.n, device="cuda") for _ in range(workers)]
+    grad = torch.empty(lay.n, device="cuda")
+    history = []
+    for _ in range(rounds):
+        total = torch.zeros((), device="cuda")
+        for k in range(workers):
+            deltas[k].zero_()
+            for _ in range(local_steps):
+                batch = torch.randn(tokens, dim, generator=g, device="cuda")
+                grad.zero_()
+                total += worker.step(driver.local[k], grad, batch, *teach(batch)).sum()
+                driver.local[k].sub_(grad, alpha=lr)            # local training ...
+                deltas[k].add_(grad, alpha=lr)                  # ... and the update it accumulates
+        driver.round(deltas)
+        history.append(total / (workers * local_steps))
+    driver.check()
+    P.train_read_status()
+    return torch.stack(history).tolist()
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--rounds", type=int, default=40)
+    ap.add_argument("--workers", type=int, default=4)
+    ap.add_argument("--dtype", choices=("f32", "bf16", "f16"), default="bf16")
+    a = ap.parse_args()
+    dtype = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[a.dtype]
+    losses = train(rounds=a.rounds, workers=a.workers, dtype=dtype)
+    for r in range(0, a.rounds, max(1, a.rounds // 10)):
+        print(f"round {r:4d}  loss {losses[r]:.4f}")
+    print(f"round {a.rounds - 1:4d}  loss {losses[-1]:.4f}")
+
+
+if __name__ == "__main__":
+    main()

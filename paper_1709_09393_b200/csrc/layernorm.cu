@@ -22,7 +22,9 @@ namespace slimdp {
 namespace {
 
 constexpr uint32_t kLnMaxParts = 1184;     // rows of partial column sums; eight CTAs on each of 148 SMs
-constexpr uint32_t kLnRowsPerPart = 8;     // fewer rows a CTA would make the partial sums a good part of the traffic
+// Rows that a CTA has at least: partial sums of fewer would be a good part of the traffic, which small inputs do not mind.
+constexpr uint32_t kLnRowsPerPart = 8, kLnRowsPerPartSmall = 4;
+constexpr uint64_t kLnSmall = 16ull << 20;     // bytes of x
 
 // Sum over the THREADS threads of a CTA, in every thread; `slot` alternates between calls that no barrier separates.
 template <int N, int THREADS>
@@ -199,6 +201,7 @@ __global__ void __launch_bounds__(GROUP == 32 ? 128 : GROUP)
     ln_backward_kernel(const T* __restrict__ dy, uint64_t lddy, const T* __restrict__ x, uint64_t ldx, uint32_t rows,
                        uint32_t dim, const float* __restrict__ gamma, const float* __restrict__ mean,
                        const float* __restrict__ rstd, T* __restrict__ dx, uint64_t lddx, float* __restrict__ parts) {
+    allow_next_kernel();
     using V = Vals<VEC>;
     constexpr int kWarps = GROUP / 32;
     constexpr bool kWarpRows = GROUP == 32;
@@ -313,6 +316,7 @@ __global__ void __launch_bounds__(GROUP, GROUP < 512 ? 512 / GROUP : 1)
                             uint32_t dim, const float* __restrict__ gamma, const float* __restrict__ mean,
                             const float* __restrict__ rstd, T* __restrict__ dx, uint64_t lddx, float* __restrict__ parts,
                             uint32_t stages) {
+    allow_next_kernel();
     constexpr int VEC = kVec<T>, kWarps = GROUP / 32;
     using V = Vals<VEC>;
     constexpr bool kKeep = GROUP < 1024;                 // 1024 threads leave no registers for gamma
@@ -457,6 +461,7 @@ __global__ void __launch_bounds__(256) ln_columns_long_kernel(const T* __restric
                                                               uint32_t dim, const float* __restrict__ mean,
                                                               const float* __restrict__ rstd,
                                                               float* __restrict__ parts) {
+    allow_next_kernel();
     const uint32_t c = blockIdx.x * 256 + threadIdx.x;
     if (c >= dim) return;
     float sh = 0.0f, s1 = 0.0f;
@@ -475,6 +480,7 @@ __global__ void __launch_bounds__(1024) ln_reduce_kernel(const float* __restrict
                                                          float* __restrict__ dgamma, float* __restrict__ dbeta,
                                                          bool accumulate) {
     __shared__ float smem[32][33];
+    wait_for_last_kernel();
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint64_t width = 2 * (uint64_t)dim, c0 = (uint64_t)blockIdx.x * 32;       // columns of a row of parts
     float s = 0.0f;
@@ -544,7 +550,7 @@ struct LnBackward {
         if (stages < kRingLeast) stages = kRingLeast, ring_ctas = kRingBytes / (kRingLeast * row_bytes);
         const bool ring = VEC > 1 && GROUP > 32 && ring_ctas > 0;
         const uint64_t most = ring ? sms * ring_ctas : std::min<uint64_t>(kLnMaxParts, sms * (1024 / threads));
-        const uint32_t ctas = (uint32_t)std::min(units, std::min(most, std::max(sms, units / kLnRowsPerPart)));
+        const uint32_t ctas = (uint32_t)std::min(units, std::min(most, std::max(sms, units / ((uint64_t)rows * dim * sizeof(T) <= kLnSmall ? kLnRowsPerPartSmall : kLnRowsPerPart))));
         *count = ctas;
         if constexpr (VEC > 1 && GROUP > 32) {
             if (ring) {
@@ -632,8 +638,8 @@ slimdp_status launch_layernorm_backward(const void* dy, uint64_t lddy, const voi
         if (s != SLIMDP_OK) return s;
     }
     if (parts) {
-        ln_reduce_kernel<<<(unsigned)((2 * (uint64_t)dim + 31) / 32), 1024, 0, st>>>(parts, count, dim, dgamma, dbeta, accumulate);
-        SLIMDP_LAUNCHED(1);
+        return launch_after(ln_reduce_kernel, dim3((unsigned)((2 * (uint64_t)dim + 31) / 32)), dim3(1024), st, parts, count, dim,
+                            dgamma, dbeta, accumulate);
     }
     return SLIMDP_OK;
 }

@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
         mbar_init_fence();
     }
-    if constexpr (P == kWeight) allow_next_kernel();
+    allow_next_kernel();
     if (warp == 1) tmem_alloc<CG>(slot, S::columns);
     tc_fence_before();
     __syncthreads();
@@ -212,6 +212,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if (warp < kFirstEpilogueWarp) {
         if constexpr (kChunked<T, P>) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoaderRegs));
         if (warp == 0) {
+            wait_for_last_kernel();              // packed operands
             uint32_t s = 0, phase = 0;
             for (uint32_t item = group; item < items && ok; item += groups) {
                 uint32_t tm, tn;
@@ -364,6 +365,7 @@ __global__ void __launch_bounds__(256) join_kernel(const ProductArgs args) {
     constexpr int PLACES = 256 / W;
     __shared__ float sums[W][V][PLACES];
     const uint32_t place = threadIdx.x % PLACES, part = threadIdx.x / PLACES;
+    wait_for_last_kernel();
     const uint64_t pieces = (args.n + V - 1) / V, total = pieces * args.m;
     for (uint64_t p0 = (uint64_t)blockIdx.x * PLACES; p0 < total; p0 += (uint64_t)gridDim.x * PLACES) {
         const uint64_t p = p0 + place, i = p / pieces, j = (p - i * pieces) * V;
@@ -406,11 +408,8 @@ template <typename T, Product P, int V>
 slimdp_status launch_join(const ProductArgs& args, cudaStream_t st) {
     const uint64_t places = (args.n + V - 1) / V * args.m, most = (uint64_t)sm_count() * 8;
     if (args.splits >= 8)
-        join_kernel<T, P, V, 8><<<(unsigned)std::min<uint64_t>((places + 31) / 32, most), 256, 0, st>>>(args);
-    else
-        join_kernel<T, P, V, 1><<<(unsigned)std::min<uint64_t>((places + 255) / 256, most), 256, 0, st>>>(args);
-    SLIMDP_LAUNCHED(1);
-    return SLIMDP_OK;
+        return launch_after(join_kernel<T, P, V, 8>, dim3((unsigned)std::min<uint64_t>((places + 31) / 32, most)), dim3(256), st, args);
+    return launch_after(join_kernel<T, P, V, 1>, dim3((unsigned)std::min<uint64_t>((places + 255) / 256, most)), dim3(256), st, args);
 }
 
 // db (+)= sum over rows of dy.  A cluster of eight CTAs takes 32 V columns, each of its 256 warps every 256th row; sums go from
@@ -426,6 +425,7 @@ __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWar
     column_sum_kernel(const T* __restrict__ dy, uint64_t lddy, uint64_t m, uint64_t n, float* __restrict__ db, bool accumulate) {
     __shared__ float smem[kSumWarps][32 * V];
     __shared__ float total[32 * V];
+    allow_next_kernel();
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = cluster_rank();
     const uint64_t j0 = (uint64_t)(blockIdx.x / kSumRanks) * 32 * V, j = j0 + lane * V;
     const uint64_t stride = kSumRanks * kSumWarps;
@@ -479,19 +479,8 @@ template <typename T>
 slimdp_status launch_column_sum(const T* dy, uint64_t lddy, uint64_t m, uint64_t n, float* db, bool accumulate, cudaStream_t st) {
     const bool wide = aligned16(dy) && (lddy * sizeof(T)) % 16 == 0;
     const uint64_t columns = wide ? 32 * kVec<T> : 32;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((n + columns - 1) / columns) * kSumRanks);
-    cfg.blockDim = dim3(32 * kSumWarps);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, wide ? column_sum_kernel<T, kVec<T>> : column_sum_kernel<T, 1>, dy, lddy, m, n, db, accumulate) != cudaSuccess)
-        return SLIMDP_ERR_CUDA;
-    SLIMDP_LAUNCHED(1);
-    return SLIMDP_OK;
+    return launch_after(wide ? column_sum_kernel<T, kVec<T>> : column_sum_kernel<T, 1>,
+                        dim3((unsigned)((n + columns - 1) / columns) * kSumRanks), dim3(32 * kSumWarps), st, dy, lddy, m, n, db, accumulate);
 }
 
 template <typename T>
@@ -536,6 +525,7 @@ struct PackJob {
 
 template <typename T>
 __global__ void __launch_bounds__(256) pack_kernel(PackJob job0, PackJob job1) {
+    allow_next_kernel();
     const PackJob job = blockIdx.y ? job1 : job0;
     const uint64_t groups = (job.cols + 7) / 8, total = groups * job.rows;
     for (uint64_t g = (uint64_t)blockIdx.x * 256 + threadIdx.x; g < total; g += (uint64_t)gridDim.x * 256) {
@@ -655,7 +645,7 @@ slimdp_status prepare_operands(Matrix& a, Matrix& b, Scratch& ws, cudaStream_t s
 
 template <typename T, Product P, int CG, int BN>
 slimdp_status launch_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, const ProductArgs& args, uint32_t groups,
-                           cudaStream_t st) {
+                           bool packed, cudaStream_t st) {
     using S = ProductShape<CG, BN>;
     static DeviceOnce once;
     auto kernel = product_kernel<T, P, CG, BN>;
@@ -673,12 +663,14 @@ slimdp_status launch_tiles(const CUtensorMap& map_a, const CUtensorMap& map_b, c
     cfg.blockDim = dim3(kProductThreads);
     cfg.dynamicSmemBytes = S::smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CG;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // as launch_after does
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = packed ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, args) != cudaSuccess) return SLIMDP_ERR_CUDA;
     SLIMDP_LAUNCHED(1);
     return SLIMDP_OK;
@@ -731,11 +723,12 @@ Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts, bool
 template <typename T, Product P>
 slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_t k, const Epilogue& e, Scratch ws,
                              cudaStream_t st, float* db = nullptr) {
-    const Matrix dy = a;
+    const Matrix first = a, second = b;
     constexpr bool kMnA = P == kWeight, kMnB = P != kForward, kF16 = sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value;
     constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
     slimdp_status s = prepare_operands<T>(a, b, ws, st);
     if (s != SLIMDP_OK) return s;
+    const bool packed = a.p != first.p || b.p != second.p;
     ProductArgs args = {};
     args.m = m;
     args.n = n;
@@ -762,14 +755,14 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
     if (sms <= 0) return SLIMDP_ERR_CUDA;
     const uint32_t groups = std::min<uint32_t>(items, (uint32_t)sms / plan.pair);
     if (plan.pair == 2 && plan.width == 256)
-        s = launch_tiles<T, P, 2, 256>(map_a, map_b, args, groups, st);
+        s = launch_tiles<T, P, 2, 256>(map_a, map_b, args, groups, packed, st);
     else if (plan.pair == 2)
-        s = launch_tiles<T, P, 2, 128>(map_a, map_b, args, groups, st);
+        s = launch_tiles<T, P, 2, 128>(map_a, map_b, args, groups, packed, st);
     else if (plan.width == 128)
-        s = launch_tiles<T, P, 1, 128>(map_a, map_b, args, groups, st);
+        s = launch_tiles<T, P, 1, 128>(map_a, map_b, args, groups, packed, st);
     else
-        s = launch_tiles<T, P, 1, 64>(map_a, map_b, args, groups, st);
-    if (s == SLIMDP_OK && db) s = launch_column_sum<T>((const T*)dy.p, dy.ld, dy.rows, dy.cols, db, e.accumulate, st);
+        s = launch_tiles<T, P, 1, 64>(map_a, map_b, args, groups, packed, st);
+    if (s == SLIMDP_OK && db) s = launch_column_sum<T>((const T*)first.p, first.ld, first.rows, first.cols, db, e.accumulate, st);
     if (s != SLIMDP_OK || args.splits == 1) return s;
     return args.wide ? launch_join<T, P, kWide<T, P>>(args, st) : launch_join<T, P, 1>(args, st);
 }

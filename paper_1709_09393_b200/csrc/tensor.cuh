@@ -134,11 +134,6 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
-// Lets the next kernel of the stream start, where it was launched so, as soon as SMs are free; and waits, in that next kernel, until
-// the one before is complete.
-__device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_last_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 // ---- tcgen05; CG = 2: the two CTAs of a pair work on one tile
 
 template <int CG>

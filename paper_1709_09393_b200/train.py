@@ -25,13 +25,25 @@ def _stream(stream, t: torch.Tensor) -> int:
     return _current_stream(t.get_device()) if stream is None else stream.cuda_stream
 
 
+def _row_stride(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name}: columns are not adjacent")
+    if rows <= 1:
+        return cols
+    if ld < cols:
+        raise ValueError(f"{name}: rows overlap")
+    return ld
+
+
 def _leading(t: torch.Tensor, name: str):
-    """The matrix that sets a call's type: (type code, dtype, shape)."""
-    code = _TYPES.get(t.dtype)
-    shape = t.shape
+    """The matrix that sets a call's type and rows: (type code, dtype, shape, address, row stride)."""
+    dtype, shape = t.dtype, t.shape
+    code = _TYPES.get(dtype)
     if code is None or not t.is_cuda or len(shape) != 2:
         raise TypeError(f"{name}: expected a 2-D CUDA tensor of float32, bfloat16 or float16")
-    return code, t.dtype, shape
+    rows, cols = shape
+    return code, dtype, shape, t.data_ptr() or None, _row_stride(t, rows, cols, name)
 
 
 def _matrix(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str):
@@ -43,14 +55,13 @@ def _matrix(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str):
         raise TypeError(f"{name}: expected a 2-D CUDA tensor of {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: expected {rows} x {cols}, got {tuple(t.shape)}")
-    ld, step = t.stride()
-    if step != 1 and cols > 1:
-        raise ValueError(f"{name}: columns are not adjacent")
-    if rows <= 1:
-        ld = cols
-    elif ld < cols:
-        raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr() or None, ld
+    return t.data_ptr() or None, _row_stride(t, rows, cols, name)
+
+
+def _width(t: torch.Tensor, at: int, name: str) -> int:
+    if t.dim() != 2:
+        raise TypeError(f"{name}: expected a 2-D CUDA tensor")
+    return t.shape[at]
 
 
 def _vector(t: Optional[torch.Tensor], n: int, name: str, dtype: torch.dtype = _F32) -> Optional[int]:
@@ -91,9 +102,8 @@ def linear_workspace_bytes(m: int, n: int, k: int, dtype: torch.dtype) -> int:
 def slimdp_layernorm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                              y: torch.Tensor, mean: Optional[torch.Tensor] = None,
                              rstd: Optional[torch.Tensor] = None, stream=None):
-    code, dtype, shape = _leading(x, "x")
+    code, dtype, shape, px, ldx = _leading(x, "x")
     rows, dim = shape
-    px, ldx = _matrix(x, shape, dtype, "x")
     py, ldy = _matrix(y, shape, dtype, "y")
     _check("slimdp_layernorm_forward",
            _lib.slimdp_layernorm_forward(px, ldx, rows, dim, code, _vector(gamma, dim, "gamma"),
@@ -105,10 +115,9 @@ def slimdp_layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional
                               rstd: torch.Tensor, dx: torch.Tensor, dgamma: Optional[torch.Tensor],
                               dbeta: Optional[torch.Tensor], ws: Optional[torch.Tensor], accumulate: bool = False,
                               stream=None):
-    code, dtype, shape = _leading(x, "x")
+    code, dtype, shape, px, ldx = _leading(x, "x")
     rows, dim = shape
     pdy, lddy = _matrix(dy, shape, dtype, "dy")
-    px, ldx = _matrix(x, shape, dtype, "x")
     pdx, lddx = _matrix(dx, shape, dtype, "dx")
     pws, nws = _ws(ws)
     _check("slimdp_layernorm_backward",
@@ -122,11 +131,10 @@ def slimdp_linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch
                           ws: torch.Tensor, activation: str = "none", residual: Optional[torch.Tensor] = None,
                           z: Optional[torch.Tensor] = None, stream=None):
     """y = act(x w^T + bias) + residual; z, if given, receives x w^T + bias."""
-    code, dtype, shape = _leading(x, "x")
+    code, dtype, shape, px, ldx = _leading(x, "x")
     act = _act(activation)
     m, k = shape
-    n = _leading(w, "w")[2][0]
-    px, ldx = _matrix(x, shape, dtype, "x")
+    n = _width(w, 0, "w")
     pw, ldw = _matrix(w, (n, k), dtype, "w")
     pr, ldr = _matrix(residual, (m, n), dtype, "residual")
     py, ldy = _matrix(y, (m, n), dtype, "y")
@@ -141,11 +149,10 @@ def slimdp_linear_backward_input(dy: torch.Tensor, w: torch.Tensor, dx: torch.Te
                                  activation: str = "none", z: Optional[torch.Tensor] = None,
                                  add: Optional[torch.Tensor] = None, stream=None):
     """dx = (dy w) * act'(z) + add, with z the pre-activation of the layer that made this one's input."""
-    code, dtype, shape = _leading(dy, "dy")
+    code, dtype, shape, pdy, lddy = _leading(dy, "dy")
     act = _act(activation)
     m, n = shape
-    k = _leading(w, "w")[2][1]
-    pdy, lddy = _matrix(dy, shape, dtype, "dy")
+    k = _width(w, 1, "w")
     pw, ldw = _matrix(w, (n, k), dtype, "w")
     pz, ldz = _matrix(z, (m, k), dtype, "z")
     pa, lda = _matrix(add, (m, k), dtype, "add")
@@ -159,10 +166,9 @@ def slimdp_linear_backward_input(dy: torch.Tensor, w: torch.Tensor, dx: torch.Te
 def slimdp_linear_backward_weight(dy: torch.Tensor, x: torch.Tensor, dw: torch.Tensor, db: Optional[torch.Tensor],
                                   ws: torch.Tensor, accumulate: bool = False, stream=None):
     """dw (+)= dy^T x in float32, db (+)= column sums of dy."""
-    code, dtype, shape = _leading(dy, "dy")
+    code, dtype, shape, pdy, lddy = _leading(dy, "dy")
     m, n = shape
-    k = _leading(x, "x")[2][1]
-    pdy, lddy = _matrix(dy, shape, dtype, "dy")
+    k = _width(x, 1, "x")
     px, ldx = _matrix(x, (m, k), dtype, "x")
     pdw, lddw = _matrix(dw, (n, k), _F32, "dw")
     pws, nws = _ws(ws)
@@ -178,10 +184,9 @@ def train_read_status(stream=None) -> None:
 
 def slimdp_activation_backward(dy: torch.Tensor, z: torch.Tensor, dz: torch.Tensor, activation: str, stream=None):
     """dz = dy * act'(z)."""
-    code, dtype, shape = _leading(dy, "dy")
+    code, dtype, shape, pdy, lddy = _leading(dy, "dy")
     act = _act(activation)
     m, n = shape
-    pdy, lddy = _matrix(dy, shape, dtype, "dy")
     pz, ldz = _matrix(z, shape, dtype, "z")
     pdz, lddz = _matrix(dz, shape, dtype, "dz")
     _check("slimdp_activation_backward",
@@ -193,9 +198,8 @@ def slimdp_distill(logits: torch.Tensor, teacher_idx: Optional[torch.Tensor], te
                    row_weight: Optional[torch.Tensor] = None, temperature: float = 1.0, kd_weight: float = 1.0,
                    ce_weight: float = 0.0, stream=None):
     """Loss of each row and its gradient; dlogits may be logits (replaced) or None (the loss alone)."""
-    code, dtype, shape = _leading(logits, "logits")
+    code, dtype, shape, pl, ldl = _leading(logits, "logits")
     rows, vocab = shape
-    pl, ldl = _matrix(logits, shape, dtype, "logits")
     pd, ldd = _matrix(dlogits, shape, dtype, "dlogits")
     if (teacher_idx is None) != (teacher_logit is None):
         raise ValueError("teacher_idx and teacher_logit come together")

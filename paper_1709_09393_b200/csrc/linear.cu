@@ -694,6 +694,7 @@ struct Shape {
     uint32_t pair, width;
     double stage, fixed, finish;
 };
+constexpr double kPowerBound = 100e3;
 constexpr Shape kShapes[] = {{2, 256, 340, 8300, 4400}, {2, 128, 180, 6500, 2200}, {1, 128, 195, 4900, 2200}, {1, 64, 165, 3800, 1100}};
 
 Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts, bool lines) {
@@ -709,6 +710,8 @@ Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts, bool
         for (uint64_t splits : {uint64_t(1), std::min<uint64_t>(most, 2), std::min<uint64_t>(most, 4), most}) {
             const double waves = (double)((tiles * splits + slots - 1) / slots), steps = (double)((kblocks + splits - 1) / splits * parts);
             double t = shape.fixed + std::max(waves * steps * stage, steps * stage + (waves - 1) * shape.finish);
+            // long products run at the power limit, where SMs without a tile in the last wave leave their share to the others
+            if (t > kPowerBound) t = shape.fixed + (double)(tiles * splits) / (double)slots * steps * stage;
             if (splits > 1) t += 2200.0 + (double)(splits * partial_bytes(m, n)) / 3700.0;
             if (best.pair == 0 || t < least) {
                 least = t;

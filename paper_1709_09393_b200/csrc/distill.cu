@@ -766,35 +766,48 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
     cluster_sync();
 }
 
-// Rows of up to 32 PIECES pieces: a warp each, its exponentials in registers, everything between its own lanes.  Sixteen such warps an SM
-// hide each other's latency without any of the slices' machinery, whose four kinds of warps meet several times a row.
-constexpr int kRowWarps = 4;
+// Rows of up to 32 WARPS PIECES pieces: WARPS warps each, their exponentials in registers; the first of them sees to the teacher's
+// entries, the label and the loss.  Sixteen such warps an SM hide each other's latency without any of the slices'
+// machinery, whose kinds of warps meet several times a row.
+constexpr int kRowWarps = 4;           // of a CTA: one row at a time, or two, or four
 
-template <typename T, int PIECES, int SECOND>
+template <typename T, int WARPS, int PIECES, int SECOND>
 __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T* logits, T* dlogits, const DistillArgs a) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, ROWS = kRowWarps / WARPS;
     extern __shared__ int32_t entries[];
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slots = table_slots(a.top), table_shift = 32 - (__ffs(slots) - 1);
-    int32_t* const s_idx = entries + warp * (4 * a.top + slots);
+    __shared__ float4 said[2][kRowWarps];          // of each warp: maximum, sums
+    __shared__ float2 coefs[2][ROWS];              // what a row's gradient is multiplied by
+    const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % WARPS, place = (threadIdx.x >> 5) / WARPS;
+    const uint32_t slots = table_slots(a.top), table_shift = 32 - (__ffs(slots) - 1);
+    const bool leading = warp == 0;
+    // the warps of a row meet at a barrier of their own
+    auto meet = [&]() {
+        if constexpr (WARPS > 1) asm volatile("bar.sync %0, %1;" ::"r"(place + 1), "n"(32 * WARPS) : "memory");
+        else __syncwarp();
+    };
+    int32_t* const s_idx = entries + place * (4 * a.top + slots);
     float* const s_t = reinterpret_cast<float*>(s_idx + a.top);
     float *const s_q = s_t + a.top, *const s_z = s_q + a.top;
     int32_t* const table = reinterpret_cast<int32_t*>(s_z + a.top);
     const uint32_t top = a.kd != 0.0f ? a.top : 0u;
     const float c_t = kLog2e / a.temperature, c_1 = kLog2e, c = a.kd != 0.0f ? c_t : c_1;
-    for (uint32_t s = lane; s < slots; s += 32) table[s] = -1;
+    if (leading)
+        for (uint32_t s = lane; s < slots; s += 32) table[s] = -1;
     __syncwarp();
-    for (uint64_t row = (uint64_t)blockIdx.x * kRowWarps + warp; row < a.rows; row += (uint64_t)gridDim.x * kRowWarps) {
+    uint32_t parity = 0;
+    for (uint64_t row = (uint64_t)blockIdx.x * ROWS + place; row < a.rows; row += (uint64_t)gridDim.x * ROWS, parity ^= 1u) {
         const T* const z = logits + row * a.ldl;
         T* const out = dlogits ? dlogits + row * a.ldd : nullptr;
         const Part p = part_of(z, a.vocab, 0, 0);
         const uint32_t tail = p.head + p.pieces * V;
-        const bool head_mine = lane < p.head, tail_mine = lane < a.vocab - tail;
+        const bool head_mine = leading && lane < p.head, tail_mine = leading && lane < a.vocab - tail;
+        auto piece_of = [&](int i) { return (i * WARPS + warp) * 32 + lane; };
         alignas(16) uint32_t raw[PIECES][4], most = Words<T>::lowest;
         float single[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             uint4 q = make_uint4(Words<T>::lowest, Words<T>::lowest, Words<T>::lowest, Words<T>::lowest);
-            if (i * 32 + lane < p.pieces) q = *reinterpret_cast<const uint4*>(z + p.head + (i * 32 + lane) * V);
+            if (piece_of(i) < p.pieces) q = *reinterpret_cast<const uint4*>(z + p.head + piece_of(i) * V);
             raw[i][0] = q.x, raw[i][1] = q.y, raw[i][2] = q.z, raw[i][3] = q.w;
         }
         if (head_mine) single[0] = to_f32(z[lane]);
@@ -803,10 +816,10 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
         const float w = a.weight ? __ldg(a.weight + row) : 1.0f;
         const int32_t y = a.label ? __ldg(a.label + row) : -1;
         const bool has_label = a.ce != 0.0f && y >= 0 && (uint32_t)y < a.vocab;
-        const float z_label = has_label ? to_f32(z[y]) : 0.0f;
+        const float z_label = leading && has_label ? to_f32(z[y]) : 0.0f;
         float tmax = -INFINITY, total = 0.0f;
         bool any = false;
-        for (uint32_t j = lane; j < top; j += 32) {
+        for (uint32_t j = lane; leading && j < top; j += 32) {
             const int32_t i = a.idx[row * a.top + j];
             const bool there = i >= 0 && (uint32_t)i < a.vocab;
             const float t = there ? load_teacher(a.teacher, a.teacher_type, row * a.top + j) : -INFINITY;
@@ -818,19 +831,21 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
         }
         const bool has_teacher = __any_sync(0xFFFFFFFFu, any);
         tmax = warp_max(tmax);
-        for (uint32_t j = lane; j < top; j += 32) total += s_q[j] = exp2_approx((s_t[j] - tmax) * c_t);
+        for (uint32_t j = lane; leading && j < top; j += 32) total += s_q[j] = exp2_approx((s_t[j] - tmax) * c_t);
         total = warp_sum(total);
-        const float coef_t = has_teacher ? w * a.kd * a.temperature : 0.0f, coef_1 = has_label ? w * a.ce : 0.0f;
+        float coef_t = has_teacher ? w * a.kd * a.temperature : 0.0f;
+        const float coef_1 = has_label ? w * a.ce : 0.0f;
 
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
             for (int u = 0; u < 4; ++u) most = Words<T>::max(most, raw[i][u]);
-        const float m_row = warp_max(fmaxf(Words<T>::top(most), fmaxf(single[0], single[1])));
-        const float m = m_row == -INFINITY ? 0.0f : m_row, off = fabsf(m) < kFar ? 0.0f : m;   // taken away first where m c does not fit
-        const float k = reference(m, c), k_1 = reference_1<SECOND>(m, c, c_1);
-        const uint64_t by2 = pair_of(c, c), k2 = pair_of(-k, -k), by2_1 = pair_of(c_1, c_1), k2_1 = pair_of(-k_1, -k_1);
-        const uint64_t less = pair_of(-off, -off);
+        const float m_w = warp_max(fmaxf(Words<T>::top(most), fmaxf(single[0], single[1])));
+        float base = m_w == -INFINITY ? 0.0f : m_w, off = fabsf(base) < kFar ? 0.0f : base;   // taken away first where m c does not fit
+        float k = reference(base, c), k_1 = reference_1<SECOND>(base, c, c_1);
+        const uint64_t by2 = pair_of(c, c), k2 = pair_of(-k, -k), by2_1 = pair_of(c_1, c_1);
+        uint64_t k2_1 = pair_of(-k_1, -k_1);
+        uint64_t less = pair_of(-off, -off);
         uint64_t e[PIECES * V / 2], sum2 = pair_of(0.0f, 0.0f), other2 = sum2;
         auto logit = [&](int i, int u) {
             const uint64_t x = Words<T>::pair(raw[i], u);
@@ -875,12 +890,39 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
         }
         sum_t = warp_sum(sum_t);
         sum_1 = SECOND != kNoSecond ? warp_sum(sum_1) : sum_t;
+        float m_row = m_w, up = 1.0f;              // the row's maximum, and what takes the warp's exponentials to it
+        if constexpr (WARPS > 1) {
+            float4* const mine = said[parity] + place * WARPS;
+            if (lane == 0) mine[warp] = make_float4(m_w, sum_t, sum_1, 0.0f);
+            if (leading && lane == 0) coefs[parity][place] = make_float2(coef_t, 0.0f);
+            meet();
+            coef_t = coefs[parity][place].x;
+            m_row = mine[0].x;
+#pragma unroll
+            for (int o = 1; o < WARPS; ++o) m_row = fmaxf(m_row, mine[o].x);
+            sum_t = sum_1 = 0.0f;
+#pragma unroll
+            for (int o = 0; o < WARPS; ++o) {
+                const float4 v = mine[o];
+                const float by = rescale(v.x, m_row, c);
+                sum_t += v.y * by;
+                if (SECOND == kOwnSecond) sum_1 += v.z * rescale(v.x, m_row, c_1);
+                if (SECOND > kOwnSecond) sum_1 += v.z * power<SECOND>(by);
+            }
+            if (SECOND == kNoSecond) sum_1 = sum_t;
+            up = rescale(m_w, m_row, c);
+            // what is computed from logits from here on is relative to the row's maximum
+            base = m_row == -INFINITY ? 0.0f : m_row, off = fabsf(base) < kFar ? 0.0f : base;
+            k = reference(base, c), k_1 = reference_1<SECOND>(base, c, c_1);
+            less = pair_of(-off, -off), k2_1 = pair_of(-k_1, -k_1);
+        }
+        const float m = base;
         // a row without a term, or with nothing but -inf, has gradient 0, whatever it holds
         const bool none = sum_t == 0.0f || (coef_t == 0.0f && coef_1 == 0.0f);
 
         float sum_q = 0.0f, term = 0.0f;
         bool shared = false;
-        if (coef_t != 0.0f) {
+        if (leading && coef_t != 0.0f) {
             for (uint32_t j = lane; j < top; j += 32)
                 if (s_idx[j] >= 0 && s_q[j] != 0.0f) {
                     sum_q += s_q[j];
@@ -894,19 +936,20 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
         if (coef_t != 0.0f) loss = a.kd * a.temperature * (term + sum_q * a.temperature * (log_sum(sum_t, m, c) - logf(total)));
         if (has_label)
             loss += a.ce * (log_sum(sum_1, m, SECOND == kOwnSecond ? c_1 : c, SECOND > kOwnSecond ? SECOND : 1) - (z_label - m));
-        if (lane == 0) a.loss[row] = none ? 0.0f : w * loss;
+        if (leading && lane == 0) a.loss[row] = none ? 0.0f : w * loss;
         if (!out) continue;
 
         const float g = none ? 0.0f : (SECOND ? coef_t : coef_t + coef_1) / sum_t, g_1 = SECOND && !none ? coef_1 / sum_1 : 0.0f;
-        const uint64_t g2 = pair_of(g, g), g2_1 = pair_of(g_1, g_1);
+        const float g_w = g * up, g_1w = g_1 * (SECOND > kOwnSecond ? power<SECOND>(up) : 1.0f);
+        const uint64_t g2 = pair_of(g_w, g_w), g2_1 = pair_of(g_1w, g_1w);
         const bool wide = (reinterpret_cast<uintptr_t>(out + p.head) & 15u) == 0;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
-            if (i * 32 + lane < p.pieces) {
+            if (piece_of(i) < p.pieces) {
                 float v[V];
                 uint64_t s[V / 2] = {};
                 if constexpr (SECOND == kOwnSecond) {     // the logits are read again: registers hold their exponentials
-                    unpack<T, V>(load_pack<T, V>(z + p.head + (i * 32 + lane) * V), v);
+                    unpack<T, V>(load_pack<T, V>(z + p.head + piece_of(i) * V), v);
 #pragma unroll
                     for (int u = 0; u < V / 2; ++u) s[u] = add_pair(pair_of(v[2 * u], v[2 * u + 1]), less);
                 }
@@ -922,7 +965,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
                 if (none)
 #pragma unroll
                     for (int u = 0; u < V; ++u) v[u] = 0.0f;
-                T* const o = out + p.head + (i * 32 + lane) * V;
+                T* const o = out + p.head + piece_of(i) * V;
                 if (wide) {
                     store_pack<T, V>(o, v);
                 } else {
@@ -930,10 +973,12 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
                     for (int u = 0; u < V; ++u) o[u] = from_f32<T>(v[u]);
                 }
             }
-        if (head_mine) out[lane] = from_f32<T>(none ? 0.0f : g * single[0] + g_1 * single_1[0]);
-        if (tail_mine) out[tail + lane] = from_f32<T>(none ? 0.0f : g * single[1] + g_1 * single_1[1]);
+        // the leading warp's own elements: their second exponential, too, is relative to the warp's maximum
+        const float g_1s = SECOND == kOwnSecond ? g_1 * rescale(m_w, m_row, c_1) : g_1w;
+        if (head_mine) out[lane] = from_f32<T>(none ? 0.0f : g_w * single[0] + g_1s * single_1[0]);
+        if (tail_mine) out[tail + lane] = from_f32<T>(none ? 0.0f : g_w * single[1] + g_1s * single_1[1]);
         // entries that share an index: found by putting the indices into a table, and only then told apart
-        if (!none && coef_t != 0.0f) {
+        if (leading && !none && coef_t != 0.0f) {
             for (uint32_t j = lane; j < top; j += 32) {
                 const int32_t i = s_idx[j];
                 if (i < 0) continue;
@@ -945,8 +990,9 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
             }
             shared = __any_sync(0xFFFFFFFFu, shared);
         }
-        __syncwarp();            // the dense result is stored; the entries go over it
-        if (!none) {
+        __syncwarp();
+        meet();                  // the dense result is stored; the entries go over it
+        if (leading && !none) {
             auto dense = [&](float v) {
                 const float x = exp2_approx(fmaf(v - off, c, -k));
                 return fmaf(g_1, second_of(v, x), g * x);
@@ -977,11 +1023,12 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T*
     }
 }
 
-template <typename T, int PIECES, int SECOND>
+template <typename T, int WARPS, int PIECES, int SECOND>
 slimdp_status launch_rows(const T* logits, T* dlogits, const DistillArgs& a, cudaStream_t st) {
     static DeviceOnce once;
-    auto kernel = distill_row_kernel<T, PIECES, SECOND>;
-    auto smem = [](uint32_t top) { return kRowWarps * (4 * top + table_slots(top)) * 4; };
+    auto kernel = distill_row_kernel<T, WARPS, PIECES, SECOND>;
+    constexpr int kRows = kRowWarps / WARPS;        // of a CTA
+    auto smem = [](uint32_t top) { return kRows * (4 * top + table_slots(top)) * 4; };
     if (once.needed()) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem(SLIMDP_MAX_TOP)) != cudaSuccess)
             return SLIMDP_ERR_CUDA;
@@ -989,7 +1036,7 @@ slimdp_status launch_rows(const T* logits, T* dlogits, const DistillArgs& a, cud
     }
     const int sms = sm_count();
     if (sms <= 0) return SLIMDP_ERR_CUDA;
-    const unsigned ctas = (unsigned)std::min<uint64_t>((a.rows + kRowWarps - 1) / kRowWarps, (uint64_t)sms * 4);
+    const unsigned ctas = (unsigned)std::min<uint64_t>((a.rows + kRows - 1) / kRows, (uint64_t)sms * 4);
     kernel<<<ctas, 32 * kRowWarps, smem(a.top), st>>>(logits, dlogits, a);
     SLIMDP_LAUNCHED(1);
     return SLIMDP_OK;
@@ -1035,8 +1082,10 @@ slimdp_status launch_slices(const T* logits, T* dlogits, const DistillArgs& a, u
 
 template <typename T, int SECOND>
 slimdp_status launch_by_length(const T* z, T* d, const DistillArgs& a, uint64_t pieces, cudaStream_t st) {
-    if (pieces <= 32 * 2) return launch_rows<T, 2, SECOND>(z, d, a, st);
-    if (pieces <= 32 * 8) return launch_rows<T, 8, SECOND>(z, d, a, st);
+    if (pieces <= 32 * 2) return launch_rows<T, 1, 2, SECOND>(z, d, a, st);
+    if (pieces <= 32 * 8) return launch_rows<T, 1, 8, SECOND>(z, d, a, st);
+    if (pieces <= 64 * 8) return launch_rows<T, 2, 8, SECOND>(z, d, a, st);
+    if (pieces <= 128 * 8) return launch_rows<T, 4, 8, SECOND>(z, d, a, st);
     for (uint32_t ranks = 1; ranks <= 8; ranks *= 2)
         if (pieces <= (uint64_t)ranks * 2048) return launch_slices<T, 8, 8, 2, SECOND>(z, d, a, ranks, st);
     return launch_slices<T, 16, 8, 1, SECOND>(z, d, a, 8, st);

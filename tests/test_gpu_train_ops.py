@@ -417,7 +417,8 @@ def test_distill(P, dtype, rows, vocab, top):
     distill_check(P, logits, idx, teacher.to(torch.float16), label, weight, 1.0, 0.5, 0.5)
 
 
-@pytest.mark.parametrize("rows,vocab,top,dtype", [(6000, 500, 6, torch.float32), (2500, 9000, 40, torch.bfloat16),
+@pytest.mark.parametrize("rows,vocab,top,dtype", [(6000, 500, 6, torch.float32), (5000, 3001, 33, torch.bfloat16),
+                                                  (3000, 4000, 12, torch.float32), (2500, 9000, 40, torch.bfloat16),
                                                   (700, 30001, 64, torch.float16), (260, 131072, 64, torch.bfloat16),
                                                   (150, 131072, 300, torch.float32), (90, 200000, 64, torch.bfloat16)])
 def test_distill_of_many_more_rows_than_run_at_once(P, rows, vocab, top, dtype):

@@ -321,7 +321,7 @@ __device__ __forceinline__ float log_sum(float sum, float m, float c, int power 
 // What is said in a cluster about a row.  A dense warp: its share's maximum and its sums relative to it, to every rank.
 // A teacher's warp: over the entries in its slice and relative to `kBase`, sum q and sum q (t - (s - base)), and the label's
 // logit, to rank 0; and to its own CTA what the row's gradient is multiplied by.
-enum { kMax, kSumT, kSum1, kVoice = 4 };
+enum { kMax, kSumT, kSum1, kPower, kVoice = 4 };     // kPower: see power_of
 enum { kBase, kQ, kTerm, kHasLabel, kLabel, kFacts = 8 };
 enum { kCoefT, kCoef1, kOwn = 4 };
 enum { kNoteTotal, kNoteLabel, kNote = 4 };     // from the first warp of the teacher's to the second
@@ -384,22 +384,39 @@ __device__ __forceinline__ float reference_1(float m, float c, float c_1) {
     return SECOND == kOwnSecond ? reference(m, c_1) : SECOND * reference(m, c);
 }
 
-// The row's maximum and sums from what all dense warps of the cluster said.
+// The power of two that a part's exponentials are short of: K where they are 2^(s c - K); for a part that adds nothing to a row
+// with an ordinary maximum (nothing but -inf, or far below), -inf.
+__device__ __forceinline__ float power_of(float m, float c) {
+    return fabsf(m) < kFar ? ceilf(m * c) : m < 0.0f ? -INFINITY : 0.0f;
+}
+
+// The row's maximum and sums from what all dense warps of the cluster said, and what takes the exponentials of a part with maximum
+// m_part and power k_part to them.
 template <int SECOND>
-__device__ __forceinline__ void row_sums(const float* said, uint32_t voices, uint32_t lane, float c, float c_1, float& m,
-                                         float& sum_t, float& sum_1) {
-    m = -INFINITY;
-    for (uint32_t i = lane; i < voices; i += 32) m = fmaxf(m, said[i * kVoice + kMax]);
+__device__ __forceinline__ float row_sums(const float* said, uint32_t voices, uint32_t lane, float c, float c_1, float m_part,
+                                          float k_part, float& m, float& sum_t, float& sum_1) {
+    float4 v[2];                                    // the first 64 voices; the largest clusters have twice as many
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+        v[u] = u * 32 + lane < voices ? *reinterpret_cast<const float4*>(said + (u * 32 + lane) * kVoice) : make_float4(-INFINITY, 0.0f, 0.0f, -INFINITY);
+    m = fmaxf(v[0].x, v[1].x);
+    for (uint32_t i = 64 + lane; i < voices; i += 32) m = fmaxf(m, said[i * kVoice + kMax]);
     m = warp_max(m);
+    const bool far = !(fabsf(m) < kFar);
+    const float k = far ? 0.0f : ceilf(m * c);
     sum_t = sum_1 = 0.0f;
-    for (uint32_t i = lane; i < voices; i += 32) {
-        const float4 v = *reinterpret_cast<const float4*>(said + i * kVoice);
-        sum_t += v.y * rescale(v.x, m, c);
-        if (SECOND == kOwnSecond) sum_1 += v.z * rescale(v.x, m, c_1);
-        if (SECOND > kOwnSecond) sum_1 += v.z * power<SECOND>(rescale(v.x, m, c));
-    }
+    auto add = [&](const float4& p) {
+        const float by = far ? rescale(p.x, m, c) : exp2_approx(p.w - k);
+        sum_t += p.y * by;
+        if (SECOND == kOwnSecond) sum_1 += p.z * rescale(p.x, m, c_1);
+        if (SECOND > kOwnSecond) sum_1 += p.z * power<SECOND>(by);
+    };
+#pragma unroll
+    for (int u = 0; u < 2; ++u) add(v[u]);
+    for (uint32_t i = 64 + lane; i < voices; i += 32) add(*reinterpret_cast<const float4*>(said + i * kVoice));
     sum_t = warp_sum(sum_t);
     sum_1 = SECOND ? warp_sum(sum_1) : sum_t;
+    return far ? rescale(m_part, m, c) : exp2_approx(k_part - k);
 }
 
 // WARPS warps turn a slice into exponentials and these into the gradient; beside them one warp prepares the teacher's
@@ -483,6 +500,7 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
                     for (int j = 0; j < PIECES; ++j)
                         if (j == i) raw[j][0] = words[0], raw[j][1] = words[1], raw[j][2] = words[2], raw[j][3] = words[3];
                 }
+            const float k_w = power_of(m_w, c);
             const uint64_t by2 = pair_of(c, c), k2 = pair_of(-reference(base, c), -reference(base, c));
             uint64_t e[S::elems / 2], sum2 = pair_of(0.0f, 0.0f), other2 = sum2;
 #pragma unroll
@@ -518,19 +536,19 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
             if constexpr (SECOND) sum_1 = warp_sum(sum_1);
             float* const said = exchange + turn % kTurns * S::said;
             if (lane < ranks)
-                send_cluster(cluster_addr(smem_addr(said + (rank * WARPS + warp) * kVoice), lane), m_w, sum_t, sum_1, 0.0f,
+                send_cluster(cluster_addr(smem_addr(said + (rank * WARPS + warp) * kVoice), lane), m_w, sum_t, sum_1, k_w,
                              cluster_addr(told(turn), lane));
             if (!(ok = mbar_wait(told(turn), (turn / kTurns) & 1u))) break;
             float m;
-            row_sums<SECOND>(said, voices, lane, c, c_1, m, sum_t, sum_1);
+            const float up = row_sums<SECOND>(said, voices, lane, c, c_1, m_w, k_w, m, sum_t, sum_1);
             const float* const own = said + 8 * WARPS * kVoice + 8 * kFacts;
             if (out) {
                 const float coef_t = own[kCoefT], coef_1 = own[kCoef1];
                 // a row without a term, or with nothing but -inf, has gradient 0, whatever it holds
                 const bool none = sum_t == 0.0f || (coef_t == 0.0f && coef_1 == 0.0f);
                 // one factor takes what the registers hold to the gradient
-                const float up = rescale(m_w, m, c), g = (SECOND ? coef_t : coef_t + coef_1) / sum_t * up;
-                const float g_1 = SECOND ? coef_1 / sum_1 * (SECOND == kOwnSecond ? 1.0f : power<SECOND>(up)) : 0.0f;
+                const float g = (SECOND ? coef_t : coef_t + coef_1) * rcp_approx(sum_t) * up;
+                const float g_1 = SECOND ? coef_1 * rcp_approx(sum_1) * (SECOND == kOwnSecond ? 1.0f : power<SECOND>(up)) : 0.0f;
                 const uint64_t g2 = pair_of(g, g), g2_1 = pair_of(g_1, g_1);
                 const float k_1 = SECOND ? -reference_1<SECOND>(m, c, c_1) : 0.0f, off_1 = fabsf(m) < kFar ? 0.0f : m;
                 // the second term, of a logit and its exponential
@@ -713,7 +731,7 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
             }
             if (!(ok = mbar_wait(told(turn), (turn / kTurns) & 1u))) break;
             float m, sum_t, sum_1;
-            row_sums<SECOND>(said, voices, lane, c, c_1, m, sum_t, sum_1);
+            row_sums<SECOND>(said, voices, lane, c, c_1, 0.0f, 0.0f, m, sum_t, sum_1);
             const float coef_t = facts[8 * kFacts + kCoefT], coef_1 = facts[8 * kFacts + kCoef1];
             const bool none = sum_t == 0.0f || (coef_t == 0.0f && coef_1 == 0.0f);
             if (m == -INFINITY) m = 0.0f;
@@ -734,8 +752,8 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
                 if (lane == 0) a.loss[row] = none ? 0.0f : w * loss;
             }
             // 2^((s - m) c) relative to the sums as they are kept
-            const float abs_t = (SECOND ? coef_t : coef_t + coef_1) / sum_t * exp2_approx(fabsf(m) < kFar ? fmaf(m, c, -ceilf(m * c)) : 0.0f);
-            const float abs_1 = SECOND ? coef_1 / sum_1 * exp2_approx(fabsf(m) < kFar ? fmaf(m, c_1, -reference_1<SECOND>(m, c, c_1)) : 0.0f) : 0.0f;
+            const float abs_t = (SECOND ? coef_t : coef_t + coef_1) * rcp_approx(sum_t) * exp2_approx(fabsf(m) < kFar ? fmaf(m, c, -ceilf(m * c)) : 0.0f);
+            const float abs_1 = SECOND ? coef_1 * rcp_approx(sum_1) * exp2_approx(fabsf(m) < kFar ? fmaf(m, c_1, -reference_1<SECOND>(m, c, c_1)) : 0.0f) : 0.0f;
             auto dense = [&](float v) {
                 const float d = abs_t * exp2_approx((v - m) * c);
                 return SECOND ? fmaf(abs_1, exp2_approx((v - m) * c_1), d) : d;

@@ -509,3 +509,84 @@ def test_distill_gradient_against_differences(P):
     along = (d.double() * u.double()).sum(1)
     # the loss is a sum of terms below 40 with a few roundings each; its third derivative along u is below |u|^3
     close(diff, along, 32 * EPS * 40 / step + step ** 2 * u.double().abs().amax(1) ** 3)
+
+
+# ------------------------------------------------------------------------------------------ all of them
+
+def test_offsets_beyond_32_bits(P):
+    """Matrices of more than 2^32 elements: the last rows are where an offset of 32 bits would land elsewhere."""
+    g = gen(77)
+    vocab = 131072
+    rows = (1 << 32) // vocab + 40
+    logits = torch.zeros(rows, vocab, device="cuda", dtype=torch.bfloat16)
+    last = matrix(24, vocab, torch.bfloat16, g, 3.0)
+    logits[-24:] = last
+    idx = torch.randint(0, vocab, (rows, 5), generator=g, device="cuda").to(torch.int32)
+    teacher = torch.randn(rows, 5, generator=g, device="cuda")
+    loss = torch.empty(rows, device="cuda")
+    P.slimdp_distill(logits, idx, teacher, loss, logits, temperature=2.0)
+    rl, tl, rd, td = R.distill(last, idx[-24:], teacher[-24:], None, None, 2.0, 1.0, 0.0)
+    close(loss[-24:], rl, tl + R.rounding(rl, torch.float32), "loss")
+    close(logits[-24:], rd, td + R.rounding(rd, torch.bfloat16), "dlogits")
+    del logits
+    dim = 4096
+    rows = (1 << 32) // dim + 100
+    x = torch.zeros(rows, dim, device="cuda", dtype=torch.bfloat16)
+    x[-50:] = matrix(50, dim, torch.bfloat16, g)
+    y = torch.empty_like(x)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    P.slimdp_layernorm_forward(x, None, None, 1e-5, y, mean, rstd)
+    ln_check(x[-50:], None, None, 1e-5, y[-50:], mean[-50:], rstd[-50:])
+    dgamma, dbeta = torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    dy = y.zero_()                                  # only the last rows have a gradient
+    dy[-50:] = matrix(50, dim, torch.bfloat16, g, 0.1)
+    dx = torch.empty_like(x)
+    P.slimdp_layernorm_backward(dy, x, None, mean, rstd, dx, dgamma, dbeta, ws_of(P.layernorm_workspace_bytes(rows, dim)))
+    rdx, rdg, rdb, _, gg, r = R.layernorm_grad(dy[-50:], x[-50:], None, mean[-50:], rstd[-50:])
+    assert ((dx[-50:].double() - rdx).norm() / rdx.norm()).item() < 2.0 ** -8
+    assert ((dgamma.double() - rdg).norm() / rdg.norm()).item() < 1e-5
+    assert ((dbeta.double() - rdb).norm() / rdb.norm()).item() < 1e-5
+    del dx, dy, y
+    w = matrix(72, dim, torch.bfloat16, g)
+    out = torch.empty(rows, 72, device="cuda", dtype=torch.bfloat16)
+    P.slimdp_linear_forward(x, w, None, out, ws_of(P.linear_workspace_bytes(rows, 72, dim, torch.bfloat16)))
+    ref, tol = R.product(x[-50:], w)
+    close(out[-50:], ref, tol + R.rounding(ref, torch.bfloat16))
+
+
+def test_calls_can_be_captured_in_a_graph(P):
+    """Every call is work on its stream alone: a captured step replays with what its buffers hold then."""
+    m, n, k, vocab = 300, 200, 136, 9000
+    g = gen(9)
+    x, w, dy, _, _ = linear_operands(m, n, k, torch.bfloat16, 3, 4)              # padded rows: packed first
+    ws = ws_of(P.linear_workspace_bytes(m, n, k, torch.bfloat16) + P.layernorm_workspace_bytes(m, k))
+    logits, idx, teacher, label, weight = distill_inputs(60, vocab, 20, torch.bfloat16, 5)
+    y, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.empty(n, k, device="cuda"), torch.empty(n, device="cuda")
+    h, dh = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+    dg, dbeta = torch.empty(k, device="cuda"), torch.empty(k, device="cuda")
+    loss, dl = torch.empty(60, device="cuda"), torch.empty_like(logits)
+
+    def step():
+        P.slimdp_layernorm_forward(x, None, None, 1e-5, h, mean, rstd)
+        P.slimdp_linear_forward(h, w, None, y, ws, activation="silu")
+        P.slimdp_linear_backward_input(dy, w, dx, ws)
+        P.slimdp_linear_backward_weight(dy, h, dw, db, ws)
+        P.slimdp_layernorm_backward(dx, x, None, mean, rstd, dh, dg, dbeta, ws)
+        P.slimdp_distill(logits, idx, teacher, loss, dl, label=label, row_weight=weight, temperature=2.0, kd_weight=0.5,
+                         ce_weight=0.5)
+
+    outs = (h, y, dx, dw, db, dh, dg, dbeta, loss, dl)
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    x.copy_(matrix(m, k, torch.bfloat16, g, 2.0))
+    logits.copy_(matrix(60, vocab, torch.bfloat16, g, 2.0))
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in outs]
+    step()
+    for a, b in zip(got, outs):
+        assert torch.equal(a, b)
+    P.train_read_status()

@@ -154,33 +154,42 @@ __global__ void __launch_bounds__(GROUP == 32 ? 128 : GROUP, GROUP == 32 ? 4 : G
 }
 
 // Rows too long for registers: the CTA walks over the row three times; the second and third walk find it in L2.
-template <typename T>
+template <typename T, int VEC>
 __global__ void __launch_bounds__(1024) ln_forward_long_kernel(const T* __restrict__ x, uint64_t ldx, uint32_t rows,
                                                                uint32_t dim, const float* __restrict__ gamma,
                                                                const float* __restrict__ beta, float eps,
                                                                T* __restrict__ y, uint64_t ldy,
                                                                float* __restrict__ mean, float* __restrict__ rstd) {
+    using V = Vals<VEC>;
     __shared__ float smem[2][1][32];
+    const uint64_t c0 = threadIdx.x * VEC;       // 64 bits: the last step may pass 2^32
     for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T* xr = x + row * ldx;
-        float s[1] = {0.0f};
-        for (uint32_t c = threadIdx.x; c < dim; c += 1024) s[0] += to_f32(xr[c]);
+        V sum = V::splat(0.0f);
+#pragma unroll 4
+        for (uint64_t c = c0; c < dim; c += 1024 * VEC) sum = sum + V::of(load_pack<T, VEC>(xr + c));
+        float s[1] = {sum.sum()};
         cta_sum<1, 1024>(s, smem, 0);
         const float mu = s[0] / (float)dim;
-        s[0] = 0.0f;
-        for (uint32_t c = threadIdx.x; c < dim; c += 1024) {
-            const float d = to_f32(xr[c]) - mu;
-            s[0] = fmaf(d, d, s[0]);
+        const V off = V::splat(-mu);
+        sum = V::splat(0.0f);
+#pragma unroll 4
+        for (uint64_t c = c0; c < dim; c += 1024 * VEC) {
+            const V d = V::of(load_pack<T, VEC>(xr + c)) + off;
+            sum = fma(d, d, sum);
         }
+        s[0] = sum.sum();
         cta_sum<1, 1024>(s, smem, 1);
         const float r = 1.0f / sqrtf(s[0] / (float)dim + eps);
         if (threadIdx.x == 0) {
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
         }
-        for (uint32_t c = threadIdx.x; c < dim; c += 1024) {
-            const float h = (to_f32(xr[c]) - mu) * r;
-            y[row * ldy + c] = from_f32<T>(fmaf(h, gamma ? __ldg(gamma + c) : 1.0f, beta ? __ldg(beta + c) : 0.0f));
+        const V by = V::splat(r);
+#pragma unroll 2
+        for (uint64_t c = c0; c < dim; c += 1024 * VEC) {
+            const V h = (V::of(load_pack<T, VEC>(xr + c)) + off) * by;
+            fma(h, parameters<VEC>(gamma, c, dim, 1.0f), parameters<VEC>(beta, c, dim, 0.0f)).store(y + row * ldy + c);
         }
     }
 }
@@ -426,53 +435,109 @@ __global__ void __launch_bounds__(GROUP, GROUP < 512 ? 512 / GROUP : 1)
             }
 }
 
-template <typename T>
+// Bytes of shared memory that the two column sums of a row take, and the most that a CTA has for them.
+template <int VEC>
+uint64_t column_bytes(uint64_t dim) { return (dim + 1024 * VEC - 1) / (1024 * VEC) * (1024 * VEC) * 8; }
+constexpr uint64_t kLnColumnBytes = 200 * 1024;
+
+// Rows whose x and dy do not fit a ring: two walks, the second finds them in L2.  COLUMNS: the column sums are kept in shared memory, each
+// by the thread that owns the column, and `parts` is written; one CTA an SM then.
+template <typename T, int VEC, bool COLUMNS>
 __global__ void __launch_bounds__(1024) ln_backward_long_kernel(const T* __restrict__ dy, uint64_t lddy,
                                                                 const T* __restrict__ x, uint64_t ldx, uint32_t rows,
                                                                 uint32_t dim, const float* __restrict__ gamma,
                                                                 const float* __restrict__ mean,
                                                                 const float* __restrict__ rstd, T* __restrict__ dx,
-                                                                uint64_t lddx) {
+                                                                uint64_t lddx, float* __restrict__ parts) {
+    using V = Vals<VEC>;
+    allow_next_kernel();
+    // accesses of WIDE sums by adjacent threads are adjacent: [piece of a thread][dy h, dy][VEC / WIDE][1024][WIDE]
+    constexpr int WIDE = VEC < 4 ? VEC : 4;
+    extern __shared__ __align__(16) float columns[];
+    auto column = [&](uint64_t c, int which, int j) {
+        return columns + ((c / (1024 * VEC) * 2 + which) * (VEC / WIDE) + j / WIDE) * 1024 * WIDE + threadIdx.x * WIDE;
+    };
+    auto add_columns = [&](uint64_t c, int which, const V& v) {
+#pragma unroll
+        for (int j = 0; j < VEC; j += WIDE) {
+            float* const at = column(c, which, j);
+            float f[WIDE];
+            unpack<float, WIDE>(load_pack<float, WIDE>(at), f);
+#pragma unroll
+            for (int i = 0; i < WIDE; ++i) f[i] += v.get(j + i);
+            store_pack<float, WIDE>(at, f);
+        }
+    };
     __shared__ float smem[2][2][32];
+    const uint64_t c0 = threadIdx.x * VEC;
+    if constexpr (COLUMNS)
+        for (uint64_t c = c0; c < dim; c += 1024 * VEC)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) column(c, 0, j)[j % WIDE] = column(c, 1, j)[j % WIDE] = 0.0f;
     int slot = 0;
     for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T *xr = x + row * ldx, *dyr = dy + row * lddy;
         const float mu = __ldg(mean + row), r = __ldg(rstd + row);
-        float s[2] = {0.0f, 0.0f};
-        for (uint32_t c = threadIdx.x; c < dim; c += 1024) {
-            const float g = to_f32(dyr[c]) * (gamma ? __ldg(gamma + c) : 1.0f);
-            s[0] += g;
-            s[1] = fmaf(g, (to_f32(xr[c]) - mu) * r, s[1]);
+        const V off = V::splat(-mu), by = V::splat(r);
+        V s0 = V::splat(0.0f), s1 = s0;
+#pragma unroll 4
+        for (uint64_t c = c0; c < dim; c += 1024 * VEC) {
+            const V h = (V::of(load_pack<T, VEC>(xr + c)) + off) * by;
+            V g = V::of(load_pack<T, VEC>(dyr + c));
+            if constexpr (COLUMNS) {
+                add_columns(c, 0, g * h);
+                add_columns(c, 1, g);
+            }
+            g = g * parameters<VEC>(gamma, c, dim, 1.0f);
+            s0 = s0 + g;
+            s1 = fma(g, h, s1);
         }
+        float s[2] = {s0.sum(), s1.sum()};
         cta_sum<2, 1024>(s, smem, slot);
         slot ^= 1;
-        const float a = s[0] / (float)dim, b = s[1] / (float)dim;
-        for (uint32_t c = threadIdx.x; c < dim; c += 1024) {
-            const float g = to_f32(dyr[c]) * (gamma ? __ldg(gamma + c) : 1.0f), h = (to_f32(xr[c]) - mu) * r;
-            dx[row * lddx + c] = from_f32<T>(r * (g - fmaf(h, b, a)));
+        const V less = V::splat(-s[0] / (float)dim), along = V::splat(-s[1] / (float)dim);
+#pragma unroll 4
+        for (uint64_t c = c0; c < dim; c += 1024 * VEC) {
+            const V h = (V::of(load_pack<T, VEC>(xr + c)) + off) * by;
+            const V g = V::of(load_pack<T, VEC>(dyr + c)) * parameters<VEC>(gamma, c, dim, 1.0f);
+            (by * (g + fma(h, along, less))).store(dx + row * lddx + c);
         }
+    }
+    if constexpr (COLUMNS) {
+        float* const part = parts + (uint64_t)blockIdx.x * 2 * dim;
+        for (uint64_t c = c0; c < dim; c += 1024 * VEC)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                part[c + j] = column(c, 0, j)[j % WIDE];
+                part[dim + c + j] = column(c, 1, j)[j % WIDE];
+            }
     }
 }
 
-// Partial column sums of rows too long for registers: CTA (x, y) takes 256 columns and every gridDim.y-th row.
-template <typename T>
+// Partial column sums of rows longer still: CTA (x, y) takes 256 VEC columns and every gridDim.y-th row.
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256) ln_columns_long_kernel(const T* __restrict__ dy, uint64_t lddy,
                                                               const T* __restrict__ x, uint64_t ldx, uint32_t rows,
                                                               uint32_t dim, const float* __restrict__ mean,
                                                               const float* __restrict__ rstd,
                                                               float* __restrict__ parts) {
+    using V = Vals<VEC>;
     allow_next_kernel();
-    const uint32_t c = blockIdx.x * 256 + threadIdx.x;
+    const uint64_t c = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * VEC;
     if (c >= dim) return;
-    float sh = 0.0f, s1 = 0.0f;
+    V sh = V::splat(0.0f), s1 = sh;
+#pragma unroll 4
     for (uint64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-        const float g = to_f32(dy[row * lddy + c]);
-        sh = fmaf(g, (to_f32(x[row * ldx + c]) - __ldg(mean + row)) * __ldg(rstd + row), sh);
-        s1 += g;
+        const V g = V::of(load_pack<T, VEC>(dy + row * lddy + c));
+        sh = fma(g, (V::of(load_pack<T, VEC>(x + row * ldx + c)) + V::splat(-__ldg(mean + row))) * V::splat(__ldg(rstd + row)), sh);
+        s1 = s1 + g;
     }
     float* part = parts + (uint64_t)blockIdx.y * 2 * dim;
-    part[c] = sh;
-    part[dim + c] = s1;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        part[c + j] = sh.get(j);
+        part[dim + c + j] = s1.get(j);
+    }
 }
 
 // Adds the rows of partial sums: 32 columns a CTA, 32 warps take every 32nd row each.
@@ -511,9 +576,9 @@ slimdp_status with_shape(uint64_t pieces, F&& f) {
     return f.template operator()<MOST, 1024>();
 }
 
-// Pieces of a thread: four of 16 bytes, or sixteen single elements.
+// Pieces of a thread: four of 16 bytes, or sixteen elements by ones or twos.
 template <int VEC>
-constexpr int kMostPieces = VEC == 1 ? 16 : 4;
+constexpr int kMostPieces = VEC >= 4 ? 4 : 16 / VEC;
 
 // Longest row that stays in the registers of 1024 threads.
 template <int VEC>
@@ -548,11 +613,12 @@ struct LnBackward {
         constexpr int per_sm = GROUP < 512 ? 512 / GROUP : 1;
         uint32_t stages = std::min(kRingMost, kRingBytes / per_sm / row_bytes), ring_ctas = per_sm;
         if (stages < kRingLeast) stages = kRingLeast, ring_ctas = kRingBytes / (kRingLeast * row_bytes);
-        const bool ring = VEC > 1 && GROUP > 32 && ring_ctas > 0;
+        constexpr bool kRing = VEC == kVec<T> && GROUP > 32;
+        const bool ring = kRing && ring_ctas > 0;
         const uint64_t most = ring ? sms * ring_ctas : std::min<uint64_t>(kLnMaxParts, sms * (1024 / threads));
         const uint32_t ctas = (uint32_t)std::min(units, std::min(most, std::max(sms, units / ((uint64_t)rows * dim * sizeof(T) <= kLnSmall ? kLnRowsPerPartSmall : kLnRowsPerPart))));
         *count = ctas;
-        if constexpr (VEC > 1 && GROUP > 32) {
+        if constexpr (kRing) {
             if (ring) {
                 auto kernel = ln_backward_ring_kernel<T, PIECES, GROUP>;
                 static DeviceOnce once;
@@ -565,7 +631,7 @@ struct LnBackward {
                 return SLIMDP_OK;
             }
         }
-        if constexpr (VEC == 1 || GROUP == 32) {
+        if constexpr (!kRing) {
             ln_backward_kernel<T, VEC, PIECES, GROUP><<<ctas, threads, 0, st>>>(dy, lddy, x, ldx, rows, dim, gamma, mean, rstd, dx, lddx, parts);
             SLIMDP_LAUNCHED(1);
             return SLIMDP_OK;
@@ -573,6 +639,34 @@ struct LnBackward {
         return SLIMDP_ERR_UNSUPPORTED;       // not reached: see backward_on_chip
     }
 };
+
+template <typename T, int VEC>
+slimdp_status launch_long(const T* dy, uint64_t lddy, const T* x, uint64_t ldx, uint32_t rows, uint32_t dim, const float* gamma,
+                          const float* mean, const float* rstd, T* dx, uint64_t lddx, float* parts, uint32_t& count, cudaStream_t st) {
+    const uint64_t sms = (uint64_t)sm_count();
+    if (parts && column_bytes<VEC>(dim) <= kLnColumnBytes) {
+        auto kernel = ln_backward_long_kernel<T, VEC, true>;
+        static DeviceOnce once;
+        if (once.needed()) {
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLnColumnBytes) != cudaSuccess) return SLIMDP_ERR_CUDA;
+            once.mark();
+        }
+        count = (uint32_t)std::min<uint64_t>(rows, std::min<uint64_t>(sms, kLnMaxParts));
+        kernel<<<count, 1024, column_bytes<VEC>(dim), st>>>(dy, lddy, x, ldx, rows, dim, gamma, mean, rstd, dx, lddx, parts);
+        SLIMDP_LAUNCHED(1);
+        return SLIMDP_OK;
+    }
+    ln_backward_long_kernel<T, VEC, false><<<(unsigned)std::min<uint64_t>(rows, sms * 2), 1024, 0, st>>>(dy, lddy, x, ldx, rows, dim, gamma, mean, rstd, dx, lddx, nullptr);
+    SLIMDP_LAUNCHED(1);
+    if (parts) {
+        // eight CTAs an SM, as far as rows and the workspace's rows of partial sums go
+        const uint64_t across = ((uint64_t)dim + 256 * VEC - 1) / (256 * VEC);
+        count = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(rows, kLnMaxParts), std::max<uint64_t>(1, sms * 8 / across));
+        ln_columns_long_kernel<T, VEC><<<dim3((unsigned)across, count), 256, 0, st>>>(dy, lddy, x, ldx, rows, dim, mean, rstd, parts);
+        SLIMDP_LAUNCHED(1);
+    }
+    return SLIMDP_OK;
+}
 
 // Whether rows stay on chip between their sums and their result; longer ones are read once more.
 bool backward_on_chip(uint64_t dim, int32_t type, bool vec) {
@@ -594,16 +688,24 @@ slimdp_status read_layernorm_status() {
 slimdp_status launch_layernorm_forward(const void* x, uint64_t ldx, uint32_t rows, uint32_t dim, int32_t type,
                                        const float* gamma, const float* beta, float eps, void* y, uint64_t ldy,
                                        float* mean, float* rstd, cudaStream_t st) {
-    const bool vec = rows_vectorise(x, ldx, dim, type) && rows_vectorise(y, ldy, dim, type);
+    auto grain = [&](uint64_t bytes) { return rows_vectorise(x, ldx, dim, type, bytes) && rows_vectorise(y, ldy, dim, type, bytes); };
     return with_type(type, [&](auto e) -> slimdp_status {
         using T = decltype(e);
         constexpr int V = kVec<T>;
-        if (vec && dim <= kLongestRow<V>)
-            return with_shape<kMostPieces<V>>((dim + V - 1) / V, LnForward<T, V>{(const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd, st});
-        if (dim <= kLongestRow<1>)
-            return with_shape<kMostPieces<1>>(dim, LnForward<T, 1>{(const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd, st});
+        auto by = [&](auto vec) {
+            constexpr int VEC = decltype(vec)::value;
+            return with_shape<kMostPieces<VEC>>((dim + VEC - 1) / VEC, LnForward<T, VEC>{(const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd, st});
+        };
+        const bool vec = grain(16);
+        if (vec && dim <= kLongestRow<V>) return by(std::integral_constant<int, V>());
+        if (!vec && dim <= kLongestRow<1>) {
+            if constexpr (sizeof(T) == 2)
+                if (grain(4)) return by(std::integral_constant<int, 2>());
+            return by(std::integral_constant<int, 1>());
+        }
         const uint32_t ctas = (uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 2);
-        ln_forward_long_kernel<T><<<ctas, 1024, 0, st>>>((const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd);
+        auto kernel = vec ? ln_forward_long_kernel<T, V> : ln_forward_long_kernel<T, 1>;
+        kernel<<<ctas, 1024, 0, st>>>((const T*)x, ldx, rows, dim, gamma, beta, eps, (T*)y, ldy, mean, rstd);
         SLIMDP_LAUNCHED(1);
         return SLIMDP_OK;
     });
@@ -613,27 +715,27 @@ slimdp_status launch_layernorm_backward(const void* dy, uint64_t lddy, const voi
                                         uint32_t dim, int32_t type, const float* gamma, const float* mean,
                                         const float* rstd, void* dx, uint64_t lddx, float* dgamma, float* dbeta,
                                         bool accumulate, void* ws, cudaStream_t st) {
-    const bool vec = rows_vectorise(x, ldx, dim, type) && rows_vectorise(dy, lddy, dim, type) && rows_vectorise(dx, lddx, dim, type);
+    auto grain = [&](uint64_t bytes) {
+        return rows_vectorise(x, ldx, dim, type, bytes) && rows_vectorise(dy, lddy, dim, type, bytes) && rows_vectorise(dx, lddx, dim, type, bytes);
+    };
+    const bool vec = grain(16);
     float* parts = (dgamma || dbeta) ? (float*)ws : nullptr;
     uint32_t count = 0;
     if (rows > 0) {
         const slimdp_status s = with_type(type, [&](auto e) -> slimdp_status {
             using T = decltype(e);
             constexpr int V = kVec<T>;
-            if (!backward_on_chip(dim, type, vec)) {
-                const uint32_t ctas = (uint32_t)std::min<uint64_t>(rows, (uint64_t)sm_count() * 2);
-                ln_backward_long_kernel<T><<<ctas, 1024, 0, st>>>((const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx);
-                SLIMDP_LAUNCHED(1);
-                if (parts) {
-                    count = std::min<uint32_t>(rows, 32);
-                    ln_columns_long_kernel<T><<<dim3((dim + 255) / 256, count), 256, 0, st>>>((const T*)dy, lddy, (const T*)x, ldx, rows, dim, mean, rstd, parts);
-                    SLIMDP_LAUNCHED(1);
-                }
-                return SLIMDP_OK;
-            }
-            if (vec)
-                return with_shape<kMostPieces<V>>((dim + V - 1) / V, LnBackward<T, V>{(const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, st, &count});
-            return with_shape<kMostPieces<1>>(dim, LnBackward<T, 1>{(const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, st, &count});
+            if (!backward_on_chip(dim, type, vec))
+                return vec ? launch_long<T, V>((const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, count, st)
+                           : launch_long<T, 1>((const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, count, st);
+            auto by = [&](auto width) {
+                constexpr int VEC = decltype(width)::value;
+                return with_shape<kMostPieces<VEC>>((dim + VEC - 1) / VEC, LnBackward<T, VEC>{(const T*)dy, lddy, (const T*)x, ldx, rows, dim, gamma, mean, rstd, (T*)dx, lddx, parts, st, &count});
+            };
+            if (vec) return by(std::integral_constant<int, V>());
+            if constexpr (sizeof(T) == 2)
+                if (grain(4)) return by(std::integral_constant<int, 2>());
+            return by(std::integral_constant<int, 1>());
         });
         if (s != SLIMDP_OK) return s;
     }

@@ -483,18 +483,38 @@ slimdp_status launch_column_sum(const T* dy, uint64_t lddy, uint64_t m, uint64_t
                         dim3((unsigned)((n + columns - 1) / columns) * kSumRanks), dim3(32 * kSumWarps), st, dy, lddy, m, n, db, accumulate);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) activation_backward_kernel(const T* __restrict__ dy, uint64_t lddy,
-                                                                  const T* __restrict__ z, uint64_t ldz, uint64_t m,
-                                                                  uint64_t n, int act, T* __restrict__ dz,
-                                                                  uint64_t lddz) {
-    for (uint64_t i = blockIdx.y; i < m; i += gridDim.y)
-        for (uint64_t j = (uint64_t)blockIdx.x * 256 + threadIdx.x; j < n; j += (uint64_t)gridDim.x * 256) {
-            const float d = to_f32(dy[i * lddy + j]);
-            float slope = 1.0f;
-            with_act(act, [&](auto a) { slope = act_slope<decltype(a)::value>(to_f32(z[i * ldz + j])); });
-            dz[i * lddz + j] = from_f32<T>(d * slope);
-        }
+// dz = dy act'(z).  2^across threads a row, each with VEC columns of `kAhead` rows at once, so that enough is on its way for the
+// bandwidth that bounds it; what a thread reads it reads before it writes there.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) activation_backward_kernel(const T* dy, uint64_t lddy, const T* z, uint64_t ldz, uint64_t m,
+                                                                  uint64_t n, int act, T* dz, uint64_t lddz, uint32_t across) {
+    constexpr int kAhead = VEC == 1 ? 8 : 4;
+    const uint32_t rows = 256u >> across;
+    const uint64_t j = (((uint64_t)blockIdx.x << across) + (threadIdx.x & ((1u << across) - 1))) * VEC;
+    if (j >= n) return;
+    for (uint64_t i = (uint64_t)blockIdx.y * rows * kAhead + (threadIdx.x >> across); i < m; i += (uint64_t)gridDim.y * rows * kAhead) {
+        Pack<T, VEC> d[kAhead], at[kAhead];
+#pragma unroll
+        for (int b = 0; b < kAhead; ++b)
+            if (i + b * rows < m) {
+                d[b] = load_pack<T, VEC>(dy + (i + b * rows) * lddy + j);
+                if (act != SLIMDP_ACT_NONE) at[b] = load_pack<T, VEC>(z + (i + b * rows) * ldz + j);
+            }
+        auto put = [&](auto&& slope) {
+#pragma unroll
+            for (int b = 0; b < kAhead; ++b)
+                if (i + b * rows < m) {
+                    float v[VEC];
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) v[c] = d[b].get(c) * slope(b, c);
+                    store_pack<T, VEC>(dz + (i + b * rows) * lddz + j, v);
+                }
+        };
+        if (act == SLIMDP_ACT_NONE)
+            put([](int, int) { return 1.0f; });
+        else
+            with_act(act, [&](auto a) { put([&](int b, int c) { return act_slope<decltype(a)::value>(at[b].get(c)); }); });
+    }
 }
 
 // ---- operands
@@ -836,10 +856,17 @@ slimdp_status launch_activation_backward(const void* dy, uint64_t lddy, const vo
                                          uint64_t n, int32_t type, int32_t act, void* dz, uint64_t lddz,
                                          cudaStream_t st) {
     if (m == 0) return SLIMDP_OK;
-    const dim3 grid((unsigned)std::min<uint64_t>((n + 255) / 256, 64), (unsigned)std::min<uint64_t>(m, 16384));
     return with_type(type, [&](auto v) -> slimdp_status {
         using T = decltype(v);
-        activation_backward_kernel<T><<<grid, 256, 0, st>>>((const T*)dy, lddy, (const T*)z, ldz, m, n, act, (T*)dz, lddz);
+        const bool vec = rows_vectorise(dy, lddy, n, type) && rows_vectorise(dz, lddz, n, type) &&
+                         (act == SLIMDP_ACT_NONE || rows_vectorise(z, ldz, n, type));
+        const uint64_t pieces = vec ? n / kVec<T> : n;
+        uint32_t across = 0;
+        while (across < 8 && (1ull << across) < pieces) ++across;
+        const uint64_t rows = (256u >> across) * (vec ? 4 : 8);
+        const dim3 grid((unsigned)((pieces + (1ull << across) - 1) >> across), (unsigned)std::min<uint64_t>((m + rows - 1) / rows, 65535));
+        auto kernel = vec ? activation_backward_kernel<T, kVec<T>> : activation_backward_kernel<T, 1>;
+        kernel<<<grid, 256, 0, st>>>((const T*)dy, lddy, (const T*)z, ldz, m, n, act, (T*)dz, lddz, across);
         SLIMDP_LAUNCHED(1);
         return SLIMDP_OK;
     });

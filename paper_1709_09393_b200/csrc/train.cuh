@@ -37,8 +37,8 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
-// N adjacent elements as one access; N sizeof(T) is 16 for a vector access and sizeof(T) for a scalar one.  Vectors of
-// 16-bit types are four words: an array of them would not stay in registers.
+// N adjacent elements as one access; N sizeof(T) is 16 for a vector access and sizeof(T) for a scalar one; two elements of a 16-bit
+// type are an access too.  Vectors of 16-bit types are words: an array of them would not stay in registers.
 template <typename T, int N>
 struct alignas(N * sizeof(T)) Pack {
     T v[N];
@@ -58,9 +58,25 @@ struct alignas(16) Pack<__half, 8> {
     }
 };
 
+template <>
+struct alignas(4) Pack<__nv_bfloat16, 2> {
+    uint32_t w;
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i % 2 ? w & 0xFFFF0000u : w << 16); }
+};
+template <>
+struct alignas(4) Pack<__half, 2> {
+    uint32_t w;
+    __device__ __forceinline__ float get(int i) const {
+        const __half2 h = *reinterpret_cast<const __half2*>(&w);
+        return i % 2 ? __high2float(h) : __low2float(h);
+    }
+};
+
 template <typename T, int N>
 __device__ __forceinline__ Pack<T, N> load_pack(const T* p) {
-    if constexpr (N * sizeof(T) == 16) {
+    if constexpr (sizeof(T) == 2 && N == 2) {
+        return {*reinterpret_cast<const uint32_t*>(p)};
+    } else if constexpr (N * sizeof(T) == 16) {
         const uint4 q = *reinterpret_cast<const uint4*>(p);
         Pack<T, N> r;
         if constexpr (sizeof(T) == 2) {
@@ -97,7 +113,9 @@ __device__ __forceinline__ uint32_t pack_two(float lo, float hi) {
 
 template <typename T, int N>
 __device__ __forceinline__ void store_pack(T* p, const float* f) {
-    if constexpr (sizeof(T) == 2 && N == 8) {
+    if constexpr (sizeof(T) == 2 && N == 2) {
+        *reinterpret_cast<uint32_t*>(p) = pack_two<T>(f[0], f[1]);
+    } else if constexpr (sizeof(T) == 2 && N == 8) {
         *reinterpret_cast<uint4*>(p) = make_uint4(pack_two<T>(f[0], f[1]), pack_two<T>(f[2], f[3]), pack_two<T>(f[4], f[5]), pack_two<T>(f[6], f[7]));
     } else {
         if constexpr (sizeof(T) == 4 && N == 4) {
@@ -246,9 +264,9 @@ __device__ __forceinline__ Vals<N> operator*(const Vals<N>& a, const Vals<N>& b)
 }
 
 // Whether every row of a matrix can be read in 16-byte pieces from its start to its end.
-inline bool rows_vectorise(const void* p, uint64_t ld, uint64_t cols, int32_t type) {
+inline bool rows_vectorise(const void* p, uint64_t ld, uint64_t cols, int32_t type, uint64_t access = 16) {
     const uint64_t b = type_bytes(type);
-    return aligned16(p) && (ld * b) % 16 == 0 && (cols * b) % 16 == 0;
+    return (uintptr_t)p % access == 0 && (ld * b) % access == 0 && (cols * b) % access == 0;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

@@ -127,6 +127,23 @@ def test_layernorm_backward(P, dtype, rows, dim):
     assert torch.equal(dbeta, once[1 + dim:1 + 2 * dim])
 
 
+# rows on 4-byte boundaries only, and rows too long for registers, for the ring or for column sums in shared memory
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,dim", [(5, 34), (333, 1002), (170, 4090), (3, 8198), (2, 16382), (400, 16390), (310, 20008),
+                                      (160, 24584), (7, 26001), (330, 30000), (3, 40000), (5, 65536)])
+def test_layernorm_of_even_and_of_long_rows(P, dtype, rows, dim):
+    test_layernorm_forward(P, dtype, rows, dim)
+    test_layernorm_backward(P, dtype, rows, dim)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad,offset", [(2, 0), (0, 2), (6, 4)])
+def test_layernorm_forward_rows_on_4_byte_boundaries(P, dtype, pad, offset):
+    for dim in (24, 1002, 4096):
+        x = matrix(11, dim, dtype, gen(dim + pad + offset), 1.0, pad, offset)
+        ln_check(x, None, None, 1e-6, *ln_forward(P, x, None, None, 1e-6, pad, offset))
+
+
 def test_layernorm_of_no_rows(P):
     x = torch.empty(0, 96, device="cuda")
     stats = torch.empty(0, device="cuda")
@@ -366,6 +383,29 @@ def test_activation_backward(P, dtype):
             assert untouched(dz, flat)
             ref = dy.double() * R.act_slope(z.double(), act)
             close(dz, ref, R.rounding(ref, dtype) + 16 * EPS * dy.double().abs() * (2 + z.double().abs()), act)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_activation_backward_in_place_and_without_z(P, dtype):
+    for m, n, pad in [(5, 3, 0), (131, 264, 8), (40, 1000, 1)]:
+        g = gen(m + 2 * n)
+        dy, z = matrix(m, n, dtype, g, 0.5, pad), matrix(m, n, dtype, g, 2.0, pad)
+        dz, _ = empty(m, n, dtype, pad)
+        P.slimdp_activation_backward(dy, z, dz, "gelu")
+        over = dy.clone()
+        P.slimdp_activation_backward(over, z, over, "gelu")
+        assert torch.equal(over, dz)
+        P.slimdp_activation_backward(dy, z, dz, "none")
+        assert torch.equal(dz, dy)
+
+
+def test_activation_backward_of_more_rows_than_a_grid_covers(P):
+    m, n = 8 * 65535 + 1003, 131
+    g = gen(5)
+    dy, z = matrix(m, n, torch.bfloat16, g), matrix(m, n, torch.bfloat16, g)
+    dz = torch.full_like(dy, -77.0)
+    P.slimdp_activation_backward(dy, z, dz, "relu")
+    assert torch.equal(dz, torch.where(z > 0, dy, torch.zeros_like(dy)))
 
 
 # ------------------------------------------------------------------------------------------ distillation

@@ -8,7 +8,13 @@
 // row, each holds a slice of at most 64 values a thread, and one exchange through distributed shared memory joins
 // maxima, sums and the loss's terms.  The few entries that have a term of their own are computed apart and stored over the
 // dense result, so that each value is rounded once.  A CTA walks over rows; the copy engine brings the slice of the
-// next row while this one is worked on.  Rows longer than a cluster holds are walked twice by one CTA.
+// next row while this one is worked on.  Rows of a warp's registers, or of four warps', need no cluster; rows longer than a
+// cluster holds are walked twice by one CTA.  Which kernel by which length: launch_by_length.
+//
+// Bound by memory where rows are long and few values are exponentials of their own (one read, one write), by the exponential unit
+// where a second softmax needs its own, and by the chain of a row's steps where rows are short.  Measured on one B200: 4096 x 131072 bf16
+// 450 us (4.8 TB/s), with labels beside the teacher at temperature 2 499 us, at temperature 3, whose second softmax has
+// exponentials of its own, 824 us; 32768 x 16384 bf16, labels alone, 366 us (5.9 TB/s); 1024 x 50021 fp16 54 us.
 #include <algorithm>
 #include <atomic>
 #include <math.h>
@@ -93,6 +99,9 @@ __device__ __forceinline__ void walk_row(const T* p, uint32_t n, Scalar&& scalar
     if (threadIdx.x < n - tail) scalar(tail + threadIdx.x);
 }
 
+// Rows longer than a cluster holds (262144 values of 16 bits, 131072 of fp32): a CTA walks over the row for its sums and again for the
+// gradient.  Bound by memory, the second walk finding part of the row in L2: 1024 x 300000 bf16 441 us, 2.8 TB/s of one read
+// and one write.
 template <typename T>
 __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const T* logits, T* dlogits, DistillArgs a) {
     constexpr int V = kVec<T>;
@@ -424,6 +433,9 @@ __device__ __forceinline__ float row_sums(const float* said, uint32_t voices, ui
 // meet at barriers in shared memory: `full` (a slice is there), `told` (an exchange is complete), `handed` (the
 // entries are prepared) and `done` (the dense result is stored).  Nothing else keeps them in step, so that the three kinds work on
 // different rows at a time.  SECOND: see kNoSecond.
+// A cluster does a row in about 6200 cycles whatever the row's length, of which the exchange and the prepared entries' way to rank 0 are
+// most; 131072 bf16 values a row make that 4.8 TB/s.  Clusters of eight find room for 33 at a time, 264 of the 296 CTAs that SMs
+// would hold.  Eight warps with two CTAs an SM against sixteen with one: 4.8 to 3.9 TB/s (2048 x 262144, which needs the sixteen, 545 us).
 template <typename T, int WARPS, int PIECES, int CTAS, int SECOND>
 __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(const T* logits, T* dlogits, const DistillArgs a) {
     using S = SliceShape<T, WARPS, PIECES>;
@@ -786,11 +798,16 @@ __global__ void __launch_bounds__(32 * WARPS + 64, CTAS) distill_slice_kernel(co
 
 // Rows of up to 32 WARPS PIECES pieces: WARPS warps each, their exponentials in registers; the first of them sees to the teacher's
 // entries, the label and the loss.  Sixteen such warps an SM hide each other's latency without any of the slices'
-// machinery, whose kinds of warps meet several times a row.
+// machinery, whose kinds of warps meet several times a row.  Bound by a row's chain of steps: its sums, the teacher's entries, its
+// stores.  Measured: 65536 x 2048 bf16 155 us with 32 entries a row (3.5 TB/s), 94 us with labels alone (5.7 TB/s), where the slices
+// take 772 and 653; 131072 x 1000 fp32 with 5 entries 230 us (4.6 TB/s); 32 x 1000 fp32 3.9 us.
 constexpr int kRowWarps = 4;           // of a CTA: one row at a time, or two, or four
+// CTAs of an SM, as registers for the exponentials allow: short rows want more of them (131072 x 500 bf16 182 us by four, 120 by eight).
+template <int PIECES>
+constexpr int kRowCtas = PIECES <= 2 ? 8 : PIECES <= 4 ? 6 : 4;
 
 template <typename T, int WARPS, int PIECES, int SECOND>
-__global__ void __launch_bounds__(32 * kRowWarps, 4) distill_row_kernel(const T* logits, T* dlogits, const DistillArgs a) {
+__global__ void __launch_bounds__(32 * kRowWarps, kRowCtas<PIECES>) distill_row_kernel(const T* logits, T* dlogits, const DistillArgs a) {
     constexpr int V = kVec<T>, ROWS = kRowWarps / WARPS;
     extern __shared__ int32_t entries[];
     __shared__ float4 said[2][kRowWarps];          // of each warp: maximum, sums
@@ -1054,7 +1071,7 @@ slimdp_status launch_rows(const T* logits, T* dlogits, const DistillArgs& a, cud
     }
     const int sms = sm_count();
     if (sms <= 0) return SLIMDP_ERR_CUDA;
-    const unsigned ctas = (unsigned)std::min<uint64_t>((a.rows + kRows - 1) / kRows, (uint64_t)sms * 4);
+    const unsigned ctas = (unsigned)std::min<uint64_t>((a.rows + kRows - 1) / kRows, (uint64_t)sms * kRowCtas<PIECES>);
     kernel<<<ctas, 32 * kRowWarps, smem(a.top), st>>>(logits, dlogits, a);
     SLIMDP_LAUNCHED(1);
     return SLIMDP_OK;
@@ -1098,9 +1115,14 @@ slimdp_status launch_slices(const T* logits, T* dlogits, const DistillArgs& a, u
     return SLIMDP_OK;
 }
 
+// The fewest warps, and of each the fewest pieces, that hold a row.  Both sides of each border, bf16, 32 entries a row, in us:
+// 131072 x 500 two pieces 120, eight 224; 131072 x 1000 four pieces 186, eight 269, by two warps 533; 65536 x 2048 one warp
+// 155, two 328, a slice 772; 32768 x 4096 two warps 152, four 179, a slice 359; 16384 x 8192 four warps 155 to 172, a slice 185.  Above, as
+// many CTAs as slices need: 4096 x 131072 by clusters 450 us, by the two walks of distill_kernel 850.
 template <typename T, int SECOND>
 slimdp_status launch_by_length(const T* z, T* d, const DistillArgs& a, uint64_t pieces, cudaStream_t st) {
     if (pieces <= 32 * 2) return launch_rows<T, 1, 2, SECOND>(z, d, a, st);
+    if (pieces <= 32 * 4) return launch_rows<T, 1, 4, SECOND>(z, d, a, st);
     if (pieces <= 32 * 8) return launch_rows<T, 1, 8, SECOND>(z, d, a, st);
     if (pieces <= 64 * 8) return launch_rows<T, 2, 8, SECOND>(z, d, a, st);
     if (pieces <= 128 * 8) return launch_rows<T, 4, 8, SECOND>(z, d, a, st);

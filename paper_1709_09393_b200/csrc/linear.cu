@@ -743,7 +743,7 @@ Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts, bool
             const double waves = (double)((tiles * splits + slots - 1) / slots), steps = (double)((kblocks + splits - 1) / splits * parts);
             double t = shape.fixed + std::max(waves * steps * stage, steps * stage + (waves - 1) * shape.finish);
             // long products run at the power limit, where SMs without a tile in the last wave leave their share to the others
-            if (t > kPowerBound) t = shape.fixed + (double)(tiles * splits) / (double)slots * steps * stage;
+            if (t > kPowerBound) t = shape.fixed + std::max(1.0, (double)(tiles * splits) / (double)slots) * steps * stage;
             if (splits > 1) t += 2200.0 + (double)(splits * partial_bytes(m, n)) / 3700.0;
             if (best.pair == 0 || t < least) {
                 least = t;

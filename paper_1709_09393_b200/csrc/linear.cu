@@ -440,8 +440,12 @@ __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWar
     const uint64_t j0 = (uint64_t)(blockIdx.x / kSumRanks) * 32 * V, j = j0 + lane * V;
     const uint64_t stride = kSumRanks * kSumWarps;
     float s[V] = {};
+    auto add = [&](const float* f) {
+#pragma unroll
+        for (int c = 0; c < V; ++c) s[c] += f[c];
+    };
+    uint64_t i = rank * kSumWarps + warp;
     if (j + V <= n) {
-        uint64_t i = rank * kSumWarps + warp;
         for (; i + (kSumAhead - 1) * stride < m; i += kSumAhead * stride) {
             Pack<T, V> p[kSumAhead];
 #pragma unroll
@@ -450,18 +454,18 @@ __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWar
             for (int u = 0; u < kSumAhead; ++u) {
                 float f[V];
                 unpack<T, V>(p[u], f);
-#pragma unroll
-                for (int c = 0; c < V; ++c) s[c] += f[c];
+                add(f);
             }
         }
-        for (; i < m; i += stride)
+    }
+    for (; i < m; i += kSumAhead * stride) {        // the last rows, and columns that are not whole pieces
+        float f[kSumAhead][V];
 #pragma unroll
-            for (int c = 0; c < V; ++c) s[c] += to_f32(dy[i * lddy + j + c]);
-    } else {
-        for (uint64_t i = rank * kSumWarps + warp; i < m; i += stride)
+        for (int u = 0; u < kSumAhead; ++u)
 #pragma unroll
-            for (int c = 0; c < V; ++c)
-                if (j + c < n) s[c] += to_f32(dy[i * lddy + j + c]);
+            for (int c = 0; c < V; ++c) f[u][c] = i + u * stride < m && j + c < n ? to_f32(dy[(i + u * stride) * lddy + j + c]) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < kSumAhead; ++u) add(f[u]);
     }
 #pragma unroll
     for (int c = 0; c < V; ++c) smem[warp][c * 32 + lane] = s[c];
@@ -485,12 +489,23 @@ __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWar
     wait_for_last_kernel();
 }
 
+// The widest pieces that rows allow and that leave work for eight clusters, else single elements: 16384 x 64 bf16 by one cluster in
+// 16-byte pieces 21.7 us, by two in single elements 5.6; 16384 x 512 10.4 by two, 6.3 by eight; 16384 x 128 fp32 24 by one, 10 by four.
 template <typename T>
 slimdp_status launch_column_sum(const T* dy, uint64_t lddy, uint64_t m, uint64_t n, float* db, bool accumulate, cudaStream_t st) {
-    const bool wide = aligned16(dy) && (lddy * sizeof(T)) % 16 == 0;
-    const uint64_t columns = wide ? 32 * kVec<T> : 32;
-    return launch_after(wide ? column_sum_kernel<T, kVec<T>> : column_sum_kernel<T, 1>,
-                        dim3((unsigned)((n + columns - 1) / columns) * kSumRanks), dim3(32 * kSumWarps), st, dy, lddy, m, n, db, accumulate);
+    constexpr uint64_t kClusters = 8;
+    auto by = [&](auto width) {
+        constexpr int V = decltype(width)::value;
+        return launch_after(column_sum_kernel<T, V>, dim3((unsigned)((n + 32 * V - 1) / (32 * V)) * kSumRanks), dim3(32 * kSumWarps), st,
+                            dy, lddy, m, n, db, accumulate);
+    };
+    auto fits = [&](uint64_t v) {
+        return (uintptr_t)dy % (v * sizeof(T)) == 0 && lddy % v == 0 && n > 32 * v * (kClusters - 1);
+    };
+    if (fits(kVec<T>)) return by(std::integral_constant<int, kVec<T>>());
+    if constexpr (sizeof(T) == 2)
+        if (fits(2)) return by(std::integral_constant<int, 2>());
+    return by(std::integral_constant<int, 1>());
 }
 
 // dz = dy act'(z).  2^across threads a row, each with VEC columns of `kAhead` rows at once, so that enough is on its way for the

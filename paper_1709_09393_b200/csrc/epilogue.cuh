@@ -22,11 +22,24 @@ constexpr uint64_t kFewRows = 8;
 
 // Whether they are to be preferred to the tensor cores, whose tiles of 128 rows would be all but empty: estimated times in us.  Measured
 // on one B200, bf16: one row of 4096 x 4096 5.1 against 13.4, five rows of 4096 x 1024 6.3 against 8.8, eight rows of
-// 16384 x 4096 67 against 27.
-inline bool few_rows(uint64_t m, uint64_t n, uint64_t k) {
+// 16384 x 4096 67 against 27.  fp32 has w packed for the tensor cores first, which alone takes longer: eight rows of 16384 x 8192 188
+// against 250, eight of 4096 x 4096 17 against 45 and more.
+inline bool few_rows(uint64_t m, uint64_t n, uint64_t k, bool fp32) {
+    if (fp32) return m <= kFewRows;
     const double rows = m <= 2 ? (double)m : m <= 4 ? 4.0 : 8.0, weight = (double)n * (double)k;
     return m <= kFewRows && 2.0 + rows * weight / 8e6 < 9.0 + weight / 3e6;
 }
+
+// Calls f with the smallest of 1, 2, 4 and 8 that is not below m, as a constant.
+template <typename F>
+slimdp_status with_rows(uint64_t m, F&& f) {
+    if (m <= 1) return f(std::integral_constant<int, 1>());
+    if (m <= 2) return f(std::integral_constant<int, 2>());
+    if (m <= 4) return f(std::integral_constant<int, 4>());
+    return f(std::integral_constant<int, 8>());
+}
+
+static_assert(kFewRows == 8, "with_rows covers all");
 
 // What the epilogue reads at V adjacent results: loaded for several places at once, before any of them is worked on.
 template <typename T, Product P, int V>

@@ -1,8 +1,9 @@
 // The forward product of up to eight rows, as single tokens make it, on the ordinary cores.
 //
 // Bound by reading w [n, k] once: warps walk over its rows in 16-byte pieces, the rows of x stay in L1.  fp32 is multiplied as it
-// is.  Sums run over the summed axis in a fixed order, so that results do not depend on scheduling.  One row of 4096 x 4096 bf16 5.1 us
-// (6.6 TB/s, partly from L2), five rows of 4096 x 1024 fp16 6.6 us; from the tensor cores 13.4 and 8.8.
+// is.  Sums run over the summed axis in a fixed order, so that results do not depend on scheduling.  One row of 16384 x 8192 fp32
+// 84 us (6.4 TB/s), bf16 45 us (5.9 TB/s); eight rows 188 and 123 us, bound by what sixteen warps an SM keep on its way.  Five
+// rows of 4096 x 1024 fp16 6.6 us.
 #include <algorithm>
 
 #include "epilogue.cuh"
@@ -38,6 +39,9 @@ __global__ void __launch_bounds__(256) few_forward_kernel(const T* __restrict__ 
                                                           uint64_t ldw, uint32_t m, uint64_t n, uint64_t k, uint32_t split,
                                                           const Epilogue e) {
     constexpr int N = M * kColumns;
+    // Two and four rows of fp32 ask for the pieces of w two steps ahead: 16384 x 8192 99 and 102 us, 145 and 138 without.  One row (108 to
+    // 85) and eight (300 to 188) are better off without, by more loads in flight and by more warps.
+    constexpr bool kTwoAhead = sizeof(T) == 4 && V > 1 && (M == 2 || M == 4);
     __shared__ float sums[8][N];
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ways = 1u << split, way = warp & (ways - 1);
     const uint64_t j0 = ((uint64_t)blockIdx.x * (8 >> split) + (warp >> split)) * kColumns;
@@ -54,11 +58,8 @@ __global__ void __launch_bounds__(256) few_forward_kernel(const T* __restrict__ 
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) acc[i][c] = Acc::splat(0.0f);
     const uint64_t pieces = k / V;
-#pragma unroll 2
-    for (uint64_t p = way * 32 + lane; p < pieces; p += ways * 32) {
-        Vals<V> a[kColumns];
-#pragma unroll
-        for (int c = 0; c < kColumns; ++c) a[c] = Vals<V>::of(load_pack<T, V>(wr[c] + p * V));
+    const uint64_t first = way * 32 + lane, step = ways * 32;
+    auto multiply = [&](const Vals<V>(&a)[kColumns], uint64_t p) {
 #pragma unroll
         for (int i = 0; i < M; ++i) {
             const Vals<V> b = Vals<V>::of(load_pack<T, V>(xr[i] + p * V));
@@ -66,6 +67,34 @@ __global__ void __launch_bounds__(256) few_forward_kernel(const T* __restrict__ 
             for (int c = 0; c < kColumns; ++c)
 #pragma unroll
                 for (int u = 0; u < (V + 1) / 2; ++u) acc[i][c].p[0] = fma_pair(a[c].p[u], b.p[u], acc[i][c].p[0]);
+        }
+    };
+    if constexpr (kTwoAhead) {
+        Pack<T, V> next[2][kColumns];
+        auto fetch = [&](int slot, uint64_t p) {
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c)
+                if (p < pieces) next[slot][c] = load_pack<T, V>(wr[c] + p * V);
+        };
+        fetch(0, first);
+        fetch(1, first + step);
+        for (uint64_t p = first; p < pieces; p += 2 * step)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                if (p + u * step < pieces) {
+                    Vals<V> a[kColumns];
+#pragma unroll
+                    for (int c = 0; c < kColumns; ++c) a[c] = Vals<V>::of(next[u][c]);
+                    fetch(u, p + (u + 2) * step);
+                    multiply(a, p + u * step);
+                }
+    } else {
+#pragma unroll 2
+        for (uint64_t p = first; p < pieces; p += step) {
+            Vals<V> a[kColumns];
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) a[c] = Vals<V>::of(load_pack<T, V>(wr[c] + p * V));
+            multiply(a, p);
         }
     }
     float v[N];
@@ -93,17 +122,6 @@ __global__ void __launch_bounds__(256) few_forward_kernel(const T* __restrict__ 
     extra[0].load(e, i, j);
     finish<T, kForward, 1, 1>(e, i, 0, 1, j, one, bias, extra);
 }
-
-// Calls f with the smallest of 1, 2, 4 and 8 that is not below m, as a constant.
-template <typename F>
-slimdp_status with_rows(uint64_t m, F&& f) {
-    if (m <= 1) return f(std::integral_constant<int, 1>());
-    if (m <= 2) return f(std::integral_constant<int, 2>());
-    if (m <= 4) return f(std::integral_constant<int, 4>());
-    return f(std::integral_constant<int, 8>());
-}
-
-static_assert(kFewRows == 8, "with_rows covers all");
 
 }  // namespace
 

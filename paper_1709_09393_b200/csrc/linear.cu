@@ -421,6 +421,39 @@ slimdp_status launch_join(const ProductArgs& args, cudaStream_t st) {
     return launch_after(join_kernel<T, P, V, 1>, dim3((unsigned)std::min<uint64_t>((places + 255) / 256, most)), dim3(256), st, args);
 }
 
+// Partial sums of dx = dy w for up to eight rows of fp32, which would not repay packing w for the tensor cores.  A thread owns V columns of dx
+// and walks down its CTA's rows of w, with the values of dy in shared memory; the join adds the CTAs' sums.  Bound by reading w: two rows
+// against 7232 x 15424 103 us with the join (4.3 TB/s), eight 109; by the tensor cores 537.
+constexpr uint32_t kFewStretch = 256;       // most rows of w of a CTA
+template <int V, int M>
+__global__ void __launch_bounds__(256) few_input_kernel(const float* __restrict__ dy, uint64_t lddy, const float* __restrict__ w,
+                                                        uint64_t ldw, uint64_t n, uint32_t stretch, const ProductArgs args) {
+    allow_next_kernel();
+    __shared__ __align__(16) float s_dy[kFewStretch * M];
+    const uint64_t first = (uint64_t)blockIdx.y * stretch, c = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * V;
+    const uint32_t count = (uint32_t)min((uint64_t)stretch, n - first);
+    for (uint32_t t = threadIdx.x; t < count * M; t += 256) {
+        const uint32_t i = t / count, j = t - i * count;
+        s_dy[j * M + i] = i < args.m ? dy[i * lddy + first + j] : 0.0f;
+    }
+    __syncthreads();
+    if (c >= args.n) return;
+    using A = Vals<V>;
+    A acc[M];
+#pragma unroll
+    for (int i = 0; i < M; ++i) acc[i] = A::splat(0.0f);
+    const float* const from = w + first * ldw + c;
+#pragma unroll 8
+    for (uint32_t j = 0; j < count; ++j) {
+        const A a = A::of(load_pack<float, V>(from + j * ldw));
+#pragma unroll
+        for (int i = 0; i < M; ++i) acc[i] = fma(a, A::splat(s_dy[j * M + i]), acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+        if (i < args.m) acc[i].store(args.partial + ((uint64_t)blockIdx.y * args.m + i) * args.ld_partial + c);
+}
+
 // db (+)= sum over rows of dy.  A cluster of eight CTAs takes 32 V columns, each of its 256 warps every 256th row; sums go from
 // registers to shared memory to rank 0, in a fixed order.  Bound by reading dy: 32 warps with eight 16-byte loads a
 // thread in flight keep an SM's share of the bandwidth busy.  It is launched after the weight's product and may start beside it, on
@@ -757,8 +790,8 @@ Plan plan_product(uint64_t m, uint64_t n, uint64_t kblocks, uint64_t parts, bool
         for (uint64_t splits : {uint64_t(1), std::min<uint64_t>(most, 2), std::min<uint64_t>(most, 4), most}) {
             const double waves = (double)((tiles * splits + slots - 1) / slots), steps = (double)((kblocks + splits - 1) / splits * parts);
             double t = shape.fixed + std::max(waves * steps * stage, steps * stage + (waves - 1) * shape.finish);
-            // long products run at the power limit, where SMs without a tile in the last wave leave their share to the others
-            if (t > kPowerBound) t = shape.fixed + std::max(1.0, (double)(tiles * splits) / (double)slots) * steps * stage;
+            // long products run at the power limit, a third slower, where SMs without a tile in the last wave leave their share to the others
+            if (t > kPowerBound) t = shape.fixed + std::max(waves, 1.3 * (double)(tiles * splits) / (double)slots) * steps * stage;
             if (splits > 1) t += 2200.0 + (double)(splits * partial_bytes(m, n)) / 3700.0;
             if (best.pair == 0 || t < least) {
                 least = t;
@@ -817,6 +850,40 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
     return args.wide ? launch_join<T, P, kWide<T, P>>(args, st) : launch_join<T, P, 1>(args, st);
 }
 
+// dx = dy w for m <= kFewRows rows of fp32: [m, n] by [n, k].
+slimdp_status launch_few_input(const float* dy, uint64_t lddy, const float* w, uint64_t ldw, uint64_t m, uint64_t n, uint64_t k,
+                               const Epilogue& e, Scratch ws, cudaStream_t st) {
+    const bool vec = rows_vectorise(w, ldw, k, SLIMDP_F32);
+    const int sms = sm_count();
+    if (sms <= 0) return SLIMDP_ERR_CUDA;
+    // eight CTAs an SM, of sixteen rows of w at least: several parts of sums take at most a third of what a packed w would, one part less
+    // than a packed x, so that the workspace holds them
+    const uint64_t across = (k + 256 * (vec ? 4 : 1) - 1) / (256 * (vec ? 4 : 1));
+    const uint64_t most = std::max<uint64_t>(1, std::min<uint64_t>(n / 16, (uint64_t)sms * 8 / across));
+    const uint64_t stretch = std::min<uint64_t>(kFewStretch, (n + most - 1) / most);
+    ProductArgs args = {};
+    args.m = m;
+    args.n = k;
+    args.e = e;
+    args.splits = (uint32_t)((n + stretch - 1) / stretch);
+    args.ld_partial = align_up(k, 8);
+    args.partial = (float*)ws.take(args.splits * m * args.ld_partial * 4);
+    const dim3 grid((unsigned)across, args.splits);
+    const slimdp_status s = with_rows(m, [&](auto rows) -> slimdp_status {
+        constexpr int M = decltype(rows)::value;
+        if (vec)
+            few_input_kernel<4, M><<<grid, 256, 0, st>>>(dy, lddy, w, ldw, n, (uint32_t)stretch, args);
+        else
+            few_input_kernel<1, M><<<grid, 256, 0, st>>>(dy, lddy, w, ldw, n, (uint32_t)stretch, args);
+        SLIMDP_LAUNCHED(1);
+        return SLIMDP_OK;
+    });
+    if (s != SLIMDP_OK) return s;
+    auto starts_wide = [&](const void* p, uint64_t ld) { return !p || (aligned16(p) && ld % 4 == 0); };
+    const bool wide = starts_wide(e.out, e.ldo) && starts_wide(e.z, e.ldz) && starts_wide(e.add, e.ldadd);
+    return wide ? launch_join<float, kInput, 4>(args, st) : launch_join<float, kInput, 1>(args, st);
+}
+
 }  // namespace
 
 size_t linear_ws_bytes(uint64_t m, uint64_t n, uint64_t k, int32_t type) {
@@ -847,7 +914,7 @@ slimdp_status launch_linear_forward(const void* x, uint64_t ldx, const void* w, 
     const Epilogue e = {bias, z, ldz, residual, ldr, y, ldy, act, false};
     return with_type(type, [&](auto v) {
         using T = decltype(v);
-        if (few_rows(m, n, k)) return launch_few_forward<T>((const T*)x, ldx, (const T*)w, ldw, m, n, k, e, st);
+        if (few_rows(m, n, k, sizeof(T) == 4)) return launch_few_forward<T>((const T*)x, ldx, (const T*)w, ldw, m, n, k, e, st);
         return launch_product<T, kForward>({x, ldx, m, k}, {w, ldw, n, k}, m, n, k, e, Scratch{(uint8_t*)ws}, st);
     });
 }
@@ -860,6 +927,9 @@ slimdp_status launch_linear_backward_input(const void* dy, uint64_t lddy, const 
     const Epilogue e = {nullptr, const_cast<void*>(z), ldz, add, ldadd, dx, lddx, act, false};
     return with_type(type, [&](auto v) {
         using T = decltype(v);
+        if constexpr (sizeof(T) == 4)
+            if (few_rows(m, n, k, true) && n <= 65535ull * kFewStretch)
+                return launch_few_input((const float*)dy, lddy, (const float*)w, ldw, m, n, k, e, Scratch{(uint8_t*)ws}, st);
         return launch_product<T, kInput>({dy, lddy, m, n}, {w, ldw, n, k}, m, k, n, e, Scratch{(uint8_t*)ws}, st);
     });
 }

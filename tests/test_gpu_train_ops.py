@@ -241,6 +241,23 @@ def test_linear_backward_input(P, dtype, m, n, k):
             close(dx, r, t + R.rounding(r, dtype), f"dx, {act}")
 
 
+# few rows against wide, tall and tiny matrices; long summed axes of few results
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (2, 1, 3000), (1, 5000, 700), (3, 40000, 36), (4, 270, 2052), (5, 33, 1030),
+                                   (7, 16, 5000), (8, 4099, 516), (8, 1000, 4096), (9, 2000, 640)])
+def test_linear_of_few_rows(P, dtype, m, n, k):
+    test_linear_forward(P, dtype, m, n, k)
+    test_linear_backward_input(P, dtype, m, n, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(40, 130, 20000), (130, 20000, 70), (20000, 70, 130)])
+def test_linear_of_long_sums_and_few_results(P, dtype, m, n, k):
+    test_linear_forward(P, dtype, m, n, k)
+    test_linear_backward_input(P, dtype, m, n, k)
+    test_linear_backward_weight(P, dtype, m, n, k)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m,n,k", LINEAR_SHAPES)
 def test_linear_backward_weight(P, dtype, m, n, k):

@@ -421,10 +421,20 @@ slimdp_status launch_join(const ProductArgs& args, cudaStream_t st) {
     return launch_after(join_kernel<T, P, V, 1>, dim3((unsigned)std::min<uint64_t>((places + 255) / 256, most)), dim3(256), st, args);
 }
 
-// Partial sums of dx = dy w for up to eight rows of fp32, which would not repay packing w for the tensor cores.  A thread owns V columns of dx
+// Partial sums of dx = dy w for up to 32 rows of fp32, which would not repay packing w for the tensor cores.  A thread owns V columns of dx
 // and walks down its CTA's rows of w, with the values of dy in shared memory; the join adds the CTAs' sums.  Bound by reading w: two rows
 // against 7232 x 15424 103 us with the join (4.3 TB/s), eight 109; by the tensor cores 537.
 constexpr uint32_t kFewStretch = 256;       // most rows of w of a CTA
+constexpr uint64_t kFewInput = 32;          // most rows of dy
+// Whether it takes the product: always up to eight rows, beyond them where w is large.  Whole calls, in us, by it and by the tensor cores: 9
+// rows against 2000 x 640 16 and 24, 22 against 3328 x 10560 91 and 146, 24 against 9600 x 256 both 23.5, 20 against 64 x 4096 19
+// and 12.5, 32 against 300 x 700 24 and 15.
+inline bool few_input(uint64_t m, uint64_t n, uint64_t k) {
+    return m <= kFewInput && n <= 65535ull * kFewStretch && (m <= kFewRows || n * k >= (m <= 16 ? 1ull << 20 : 1ull << 22));
+}
+// Columns of a thread: the sums of more rows leave registers for fewer.
+template <int M>
+constexpr int kFewColumns = M <= 16 ? 4 : 2;
 template <int V, int M>
 __global__ void __launch_bounds__(256) few_input_kernel(const float* __restrict__ dy, uint64_t lddy, const float* __restrict__ w,
                                                         uint64_t ldw, uint64_t n, uint32_t stretch, const ProductArgs args) {
@@ -464,7 +474,7 @@ constexpr uint32_t kSumRanks = 8, kSumWarps = 32;
 constexpr int kSumAhead = 8;
 
 template <typename T, int V>
-__global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWarps)
+__global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWarps, V == 1 ? 2 : 1)
     column_sum_kernel(const T* __restrict__ dy, uint64_t lddy, uint64_t m, uint64_t n, float* __restrict__ db, bool accumulate) {
     __shared__ float smem[kSumWarps][32 * V];
     __shared__ float total[32 * V];
@@ -490,15 +500,22 @@ __global__ void __cluster_dims__(kSumRanks, 1, 1) __launch_bounds__(32 * kSumWar
                 add(f);
             }
         }
+#pragma unroll 4
+        for (; i < m; i += stride) {
+            float f[V];
+            unpack<T, V>(load_pack<T, V>(dy + i * lddy + j), f);
+            add(f);
+        }
     }
-    for (; i < m; i += kSumAhead * stride) {        // the last rows, and columns that are not whole pieces
-        float f[kSumAhead][V];
+    constexpr int kRest = V == 1 ? kSumAhead : 2;
+    for (; i < m && j < n; i += kRest * stride) {   // columns that are not whole pieces
+        float f[kRest][V];
 #pragma unroll
-        for (int u = 0; u < kSumAhead; ++u)
+        for (int u = 0; u < kRest; ++u)
 #pragma unroll
             for (int c = 0; c < V; ++c) f[u][c] = i + u * stride < m && j + c < n ? to_f32(dy[(i + u * stride) * lddy + j + c]) : 0.0f;
 #pragma unroll
-        for (int u = 0; u < kSumAhead; ++u) add(f[u]);
+        for (int u = 0; u < kRest; ++u) add(f[u]);
     }
 #pragma unroll
     for (int c = 0; c < V; ++c) smem[warp][c * 32 + lane] = s[c];
@@ -850,16 +867,16 @@ slimdp_status launch_product(Matrix a, Matrix b, uint64_t m, uint64_t n, uint64_
     return args.wide ? launch_join<T, P, kWide<T, P>>(args, st) : launch_join<T, P, 1>(args, st);
 }
 
-// dx = dy w for m <= kFewRows rows of fp32: [m, n] by [n, k].
+// dx = dy w for m <= kFewInput rows of fp32: [m, n] by [n, k].
 slimdp_status launch_few_input(const float* dy, uint64_t lddy, const float* w, uint64_t ldw, uint64_t m, uint64_t n, uint64_t k,
                                const Epilogue& e, Scratch ws, cudaStream_t st) {
     const bool vec = rows_vectorise(w, ldw, k, SLIMDP_F32);
     const int sms = sm_count();
     if (sms <= 0) return SLIMDP_ERR_CUDA;
-    // eight CTAs an SM, of sixteen rows of w at least: several parts of sums take at most a third of what a packed w would, one part less
-    // than a packed x, so that the workspace holds them
-    const uint64_t across = (k + 256 * (vec ? 4 : 1) - 1) / (256 * (vec ? 4 : 1));
-    const uint64_t most = std::max<uint64_t>(1, std::min<uint64_t>(n / 16, (uint64_t)sms * 8 / across));
+    // eight CTAs an SM, of sixteen rows of w or twice as many as of dy at least: several parts of sums take at most a third of what a packed w
+    // would, one part less than a packed x, so that the workspace holds them
+    const uint64_t columns = 256 * (!vec ? 1 : m <= 16 ? kFewColumns<16> : kFewColumns<32>), across = (k + columns - 1) / columns;
+    const uint64_t most = std::max<uint64_t>(1, std::min<uint64_t>(n / std::max<uint64_t>(16, 2 * m), (uint64_t)sms * 8 / across));
     const uint64_t stretch = std::min<uint64_t>(kFewStretch, (n + most - 1) / most);
     ProductArgs args = {};
     args.m = m;
@@ -869,15 +886,18 @@ slimdp_status launch_few_input(const float* dy, uint64_t lddy, const float* w, u
     args.ld_partial = align_up(k, 8);
     args.partial = (float*)ws.take(args.splits * m * args.ld_partial * 4);
     const dim3 grid((unsigned)across, args.splits);
-    const slimdp_status s = with_rows(m, [&](auto rows) -> slimdp_status {
+    auto launch = [&](auto rows) -> slimdp_status {
         constexpr int M = decltype(rows)::value;
         if (vec)
-            few_input_kernel<4, M><<<grid, 256, 0, st>>>(dy, lddy, w, ldw, n, (uint32_t)stretch, args);
+            few_input_kernel<kFewColumns<M>, M><<<grid, 256, 0, st>>>(dy, lddy, w, ldw, n, (uint32_t)stretch, args);
         else
             few_input_kernel<1, M><<<grid, 256, 0, st>>>(dy, lddy, w, ldw, n, (uint32_t)stretch, args);
         SLIMDP_LAUNCHED(1);
         return SLIMDP_OK;
-    });
+    };
+    const slimdp_status s = m <= kFewRows ? with_rows(m, launch)
+                            : m <= 16     ? launch(std::integral_constant<int, 16>())
+                                          : launch(std::integral_constant<int, 32>());
     if (s != SLIMDP_OK) return s;
     auto starts_wide = [&](const void* p, uint64_t ld) { return !p || (aligned16(p) && ld % 4 == 0); };
     const bool wide = starts_wide(e.out, e.ldo) && starts_wide(e.z, e.ldz) && starts_wide(e.add, e.ldadd);
@@ -928,7 +948,7 @@ slimdp_status launch_linear_backward_input(const void* dy, uint64_t lddy, const 
     return with_type(type, [&](auto v) {
         using T = decltype(v);
         if constexpr (sizeof(T) == 4)
-            if (few_rows(m, n, k, true) && n <= 65535ull * kFewStretch)
+            if (few_input(m, n, k))
                 return launch_few_input((const float*)dy, lddy, (const float*)w, ldw, m, n, k, e, Scratch{(uint8_t*)ws}, st);
         return launch_product<T, kInput>({dy, lddy, m, n}, {w, ldw, n, k}, m, k, n, e, Scratch{(uint8_t*)ws}, st);
     });

@@ -33,7 +33,7 @@ __device__ __forceinline__ float warp_sums(float (&v)[N], uint32_t lane) {
 }
 
 // y = act(x w^T + bias) + residual: a warp makes M x 4 dot products over every (1 << split)-th stretch of 32 pieces; the warps
-// of a CTA that share outputs add theirs.  16-byte pieces where the rows allow, else single elements.
+// of a CTA that share outputs add theirs.  16-byte pieces where the rows allow, else pairs or single elements.
 template <typename T, int V, int M>
 __global__ void __launch_bounds__(256) few_forward_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w,
                                                           uint64_t ldw, uint32_t m, uint64_t n, uint64_t k, uint32_t split,
@@ -128,8 +128,14 @@ __global__ void __launch_bounds__(256) few_forward_kernel(const T* __restrict__ 
 template <typename T>
 slimdp_status launch_few_forward(const T* x, uint64_t ldx, const T* w, uint64_t ldw, uint64_t m, uint64_t n, uint64_t k,
                                  const Epilogue& e, cudaStream_t st) {
-    const bool wide = aligned16(x) && aligned16(w) && (ldw * sizeof(T)) % 16 == 0 && (m == 1 || (ldx * sizeof(T)) % 16 == 0);
-    const uint64_t warps = (n + kColumns - 1) / kColumns, stretches = (wide ? k / kVec<T> : k) / 32;
+    auto fits = [&](uint64_t v) {        // rows of pieces of v elements
+        const uint64_t bytes = v * sizeof(T);
+        return (uintptr_t)x % bytes == 0 && (uintptr_t)w % bytes == 0 && (n == 1 || ldw % v == 0) && (m == 1 || ldx % v == 0);
+    };
+    // Rows of a 16-bit type on 4-byte boundaries go by pairs, up to four of them: two rows of 14665 x 9492 bf16 121 us, 237 by single
+    // elements, one of 4096 x 4098 29 and 61; eight of 4096 x 1002 would take 30, 17.5 by single elements.
+    const bool wide = fits(kVec<T>), twos = sizeof(T) == 2 && !wide && m <= 4 && fits(2);
+    const uint64_t warps = (n + kColumns - 1) / kColumns, stretches = k / (wide ? kVec<T> : twos ? 2 : 1) / 32;
     const int sms = sm_count();
     if (sms <= 0) return SLIMDP_ERR_CUDA;
     // more warps an output only while there are fewer than eight an SM and each has a stretch
@@ -140,7 +146,9 @@ slimdp_status launch_few_forward(const T* x, uint64_t ldx, const T* w, uint64_t 
         constexpr int M = decltype(rows)::value;
         if (wide)
             few_forward_kernel<T, kVec<T>, M><<<ctas, 256, 0, st>>>(x, ldx, w, ldw, (uint32_t)m, n, k, split, e);
-        else
+        else if (twos) {
+            if constexpr (sizeof(T) == 2 && M <= 4) few_forward_kernel<T, 2, M><<<ctas, 256, 0, st>>>(x, ldx, w, ldw, (uint32_t)m, n, k, split, e);
+        } else
             few_forward_kernel<T, 1, M><<<ctas, 256, 0, st>>>(x, ldx, w, ldw, (uint32_t)m, n, k, split, e);
         SLIMDP_LAUNCHED(1);
         return SLIMDP_OK;

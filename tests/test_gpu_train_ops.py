@@ -245,7 +245,8 @@ def test_linear_backward_input(P, dtype, m, n, k):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (2, 1, 3000), (1, 5000, 700), (3, 40000, 36), (4, 270, 2052), (5, 33, 1030),
                                    (7, 16, 5000), (8, 4099, 516), (8, 1000, 4096), (9, 2000, 640), (16, 700, 1028),
-                                   (17, 5001, 516), (32, 3000, 260), (31, 333, 77), (33, 400, 300)])
+                                   (17, 5001, 516), (32, 3000, 260), (31, 333, 77), (33, 400, 300), (1, 700, 4098),
+                                   (2, 333, 1002), (4, 1000, 94), (5, 600, 1002)])
 def test_linear_of_few_rows(P, dtype, m, n, k):
     test_linear_forward(P, dtype, m, n, k)
     test_linear_backward_input(P, dtype, m, n, k)
